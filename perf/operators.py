@@ -458,9 +458,8 @@ def _plain_admit(s):
     block[:, 0] = s["anchors"]
     st["block_tok"][slots] = torch.where(ok[:, None], block, st["block_tok"][slots].long()).int()
     st["ctx_len"][slots] = torch.where(ok, lens, st["ctx_len"][slots].long()).int()
-    for name in ("n_ver", "q_row0"):
+    for name in ("n_ver", "q_row0", "slot_status"):
         st[name][slots] = torch.where(ok, 0, st[name][slots])
-    st["slot_status"][slots] = torch.where(ok, 0, 1).int()
     st["active"][slots] = torch.where(ok, 1, st["active"][slots]).to(torch.uint8)
     st["free_top"].copy_(top - torch.where(ok, want, 0).sum())
 
