@@ -65,6 +65,10 @@ extern "C" {
 #define ISD_ST_NONFINITE_LOGIT 16u /* NaN or +inf logit (-inf is legal)               */
 #define ISD_ST_EMPTY_RESIDUAL 32u /* informational: residual max(0,p-q) was empty in
                                      fp32, token drawn from p instead; not an error  */
+#define ISD_ST_BAD_SLOT 64u       /* isd_admit, in result[i] only: slot id out of range, in
+                                     use already, or named twice in the call             */
+#define ISD_ST_MAP_FULL 128u      /* isd_admit, in result[i] only: the request's tokens do
+                                     not fit into the maps                               */
 #define ISD_ST_KERNEL_TIMEOUT 0x80000000u /* a wait inside a kernel (on a shared-memory
                                      barrier or on another CTA's readiness counter) outlasted
                                      its time limit (isd_set_wait_limit): the CTA stopped
@@ -287,6 +291,134 @@ typedef struct isd_lora_args {
  * 256, or when t has more 128 x 256 blocks than the GPU has SMs), no allocation, no synchronisation.
  */
 int isd_lora_linear(isd_ctx* ctx, const isd_lora_args* args, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A KV cache held in 4 bits (the paper has no counterpart: its serving tables keep the cache in bf16).
+ *
+ * One pool holds keys and values, kv_pool [num_pages, Hkv, ISD_QUANT_TILE_BYTES] bytes.  The tile of a
+ * (page, kv head):
+ *   bytes [0, 1024)     K codes, 32-bit words [4 chunks of 32 dims][16 tokens][4]; a word holds eight
+ *                       consecutive dims of one token
+ *   bytes [1024, 2048)  V codes, 32-bit words [128 dims][2]; a word holds eight consecutive tokens of
+ *                       one dim
+ *   bytes [2048, 2176)  bf16: K scale[16], K zero[16], V scale[16], V zero[16] (one per token; "zero"
+ *                       holds the number 128 + z)
+ * In a word, element 2i occupies bits 4i..4i+3 and element 2i+1 bits 16+4i..16+4i+3.
+ *
+ * Codec of the 128 values x of one (token, head), K and V alike (round = to nearest, ties to even):
+ *   lo = min(0, min x), hi = max(0, max x)
+ *   s  = bf16(f32(f32(hi - lo) / 15)), z = clamp(round(f32(-lo / s)), 0, 15)
+ *   c  = clamp(round(f32(x / s)) + z, 0, 15), standing for the value s * (c - z)
+ * s = 0 (all values zero, or too small) stores zeros; a NaN or infinity in x, or a range that overflows,
+ * stores s = NaN, so that whoever attends to the token sees NaN, as with the bf16 cache.  One group per
+ * (token, head): the scale is then a factor of a key's column of scores and of a key's probability, so
+ * that the tensor cores multiply the integers c - z (exact in bf16) and every scale stays in fp32.
+ * ---------------------------------------------------------------------------------------------- */
+#define ISD_QUANT_TILE_BYTES 2176
+
+/*
+ * isd_attn over the 4-bit cache: same computation, masks, state, outputs and faults as isd_attn, on
+ * `kv_pool` in place of k_pool / v_pool.  The block's rows of k_new / v_new (bf16) are quantised and
+ * written into the slot's pages first, and are attended to as the cache holds them; tokens of the last
+ * page behind the block are emptied (scale 0).  Scores, softmax statistics and accumulation are fp32;
+ * a probability times its value scale is rounded to bf16 once, as the tensor cores' operand.
+ */
+int isd_attn_quant(isd_ctx* ctx, const isd_batch_state* st, const void* q, const void* k_new,
+                   const void* v_new, void* kv_pool, void* attn_out, float* attn_lse, void* cuda_stream);
+
+/* One layer's share of a step on the 4-bit cache (see isd_layer_args). */
+typedef struct isd_quant_layer_args {
+  const void* q;
+  const void* k_new;
+  const void* v_new;
+  void* kv_pool;
+  void* attn_out;
+  float* attn_lse; /* or NULL */
+} isd_quant_layer_args;
+
+/* isd_step_layers on the 4-bit cache: isd_attn_quant for each of the n_layers >= 1 layers, then
+ * verification and commit.  May be captured into a CUDA graph like isd_step_layers. */
+int isd_step_quant(isd_ctx* ctx, isd_batch_state* st, const isd_quant_layer_args* layers, int32_t n_layers,
+                   const void* logits_cur, const void* q_prev_logits, const isd_verify_out* out,
+                   uint64_t step, void* cuda_stream);
+
+/* Rows of tokens and where their slots are in the 4-bit cache. */
+typedef struct isd_kv_quant_args {
+  void* k;                 /* [n_tokens, Hkv, 128] bf16; rows k_row_stride elements apart        */
+  void* v;                 /* same shape                                                         */
+  int64_t k_row_stride;    /* elements, a multiple of 8, at least Hkv * 128                      */
+  int64_t v_row_stride;
+  const int64_t* slot_map; /* [n_tokens] page * 16 + offset in the page; < 0: padding, skipped   */
+  void* kv_pool;           /* [num_pages, Hkv, ISD_QUANT_TILE_BYTES]                             */
+  int64_t n_tokens;        /* >= 0                                                               */
+} isd_kv_quant_args;
+
+/*
+ * Write the keys and values of prompt tokens into the 4-bit cache (Sec. 3.3 (2): the prefill's KV rows
+ * enter the paged cache by one batched scatter) / read tokens back as bf16 (each value rounded once).
+ * The order of slot_map is free; runs of consecutive slots, as isd_admit makes them, are the fast case.
+ * No slot may occur twice in one write (the two tokens' codes would mix; nothing else is harmed).
+ * A read leaves the rows of padding entries as they were.  Entries at or above num_pages * 16 are skipped
+ * and set ISD_ST_BAD_PAGE_ID in the global status word.
+ */
+int isd_kv_write_quant(isd_ctx* ctx, const isd_kv_quant_args* args, void* cuda_stream);
+int isd_kv_read_quant(isd_ctx* ctx, const isd_kv_quant_args* args, void* cuda_stream);
+
+/* Requests that enter free slots; all pointers are device pointers. */
+typedef struct isd_admit_args {
+  const int32_t* slots;    /* [n] slot of request i; inactive before the call                    */
+  const int32_t* lens;     /* [n] tokens whose KV will be cached (the prompt without its last
+                              token, which is the anchor); >= 0                                  */
+  const int32_t* anchors;  /* [n] last token of the prompt: row 0 of the slot's first block      */
+  int32_t* result;         /* [n] 0 = admitted, else ISD_ST_* bits                               */
+  int32_t* cu_len;         /* [n + 1] tokens of the admitted requests before request i           */
+  int64_t* slot_map;       /* [map_cap] page * 16 + offset of token t, or NULL                   */
+  int32_t* tok_req;        /* [map_cap] request index of token t, or NULL                        */
+  int32_t* tok_pos;        /* [map_cap] position of token t in its request, or NULL              */
+  int64_t map_cap;         /* room in the three maps, 0 .. 2^31 - 1                              */
+  int32_t n;               /* >= 0                                                               */
+} isd_admit_args;
+
+/*
+ * Admission, the counterpart of isd_release (Sec. 3.3 (2): requests join the stationary batch without a
+ * round trip to the host).  Request i takes ceil((lens[i] + Q) / page_size) pages from the free stack:
+ * requests ascending, logical pages ascending, entry free_stack[free_top - 1 - k] for the k-th page
+ * asked for.  Requests are served while pages and room in the maps last, so those served are a prefix of
+ * the valid ones.  An admitted slot gets its page table entries, ctx_len = lens[i], n_ver = 0,
+ * q_row0 = 0, block_tok = [anchor, MASK ...], slot_status = 0 and active = 1; the maps list the
+ * admitted requests' tokens in order (token t of request i is at cu_len[i] + position), entries from
+ * cu_len[n] on stay as they were.  A request that is not admitted changes nothing but result[i]:
+ * ISD_ST_BAD_SLOT, ISD_ST_SLOT_CAPACITY (negative length, or more than max_pages_per_slot pages),
+ * ISD_ST_POOL_EXHAUSTED or ISD_ST_MAP_FULL.  Of two requests for one slot the first counts.
+ */
+int isd_admit(isd_ctx* ctx, isd_batch_state* st, const isd_admit_args* args, void* cuda_stream);
+
+#define ISD_MAX_TOP_LOGPROBS 32
+
+/* Log probabilities of given tokens; all pointers are device pointers. */
+typedef struct isd_logprobs_args {
+  const void* logits;      /* [logits_rows, V] in the context's dtype and vocabulary             */
+  int64_t logits_rows;
+  const int32_t* rows;     /* [n] row of logits judged by entry i, or NULL: row i                */
+  const int32_t* tokens;   /* [n] given token; < 0: the entry is skipped, its row not read       */
+  int32_t n;               /* >= 0                                                               */
+  int32_t top_n;           /* alternatives to report, 0 .. min(V, ISD_MAX_TOP_LOGPROBS)          */
+  float* logprob;          /* [n] log softmax(row * invT)[token]                                 */
+  float* entropy;          /* [n] -sum p log p of the row's law, or NULL                         */
+  int32_t* top_id;         /* [n, top_n] most likely tokens, best first, lower index on ties     */
+  float* top_logprob;      /* [n, top_n]                                                         */
+} isd_logprobs_args;
+
+/*
+ * What a serving front end reports beside the tokens isd_verify emitted (the paper's evaluation harness
+ * scores with them): natural-log probability of a given token under the law softmax(row *
+ * inv_temperature), that law's entropy and its top_n alternatives, from one pass over the row.  Skipped
+ * entries get NaN and id -1.  A token >= vocab or a row index outside [0, logits_rows) does the same and
+ * sets ISD_ST_BAD_TOKEN_ID; a NaN or +inf logit in a row does the same and sets ISD_ST_NONFINITE_LOGIT
+ * (in the global status word).  -inf is legal: probability zero, log probability -inf; a row of nothing
+ * but -inf is reported like a row with a NaN.
+ */
+int isd_logprobs(isd_ctx* ctx, const isd_logprobs_args* args, void* cuda_stream);
 
 /* Off the hot path: return the pages of finished slots (device array `slots`
  * of n ids) to the free stack and mark them inactive. */

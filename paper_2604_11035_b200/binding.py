@@ -16,11 +16,15 @@ LIB_PATH = os.path.join(_HERE, "libisd.so")
 
 ST_POOL_EXHAUSTED, ST_SLOT_CAPACITY, ST_BAD_TOKEN_ID = 1, 2, 4
 ST_BAD_PAGE_ID, ST_NONFINITE_LOGIT, ST_EMPTY_RESIDUAL = 8, 16, 32
+ST_BAD_SLOT, ST_MAP_FULL = 64, 128
 ST_KERNEL_TIMEOUT = 0x80000000
+QUANT_TILE_BYTES = 2176
+MAX_TOP_LOGPROBS = 32
 
 EXPORTS = ["isd_create", "isd_destroy", "isd_attn", "isd_verify", "isd_commit", "isd_step",
            "isd_release", "isd_read_status", "isd_set_profile_events", "isd_launch_count", "isd_strerror",
            "isd_verify_static", "isd_step_layers", "isd_set_step_counter", "isd_lora_linear", "isd_set_wait_limit",
+           "isd_attn_quant", "isd_step_quant", "isd_kv_write_quant", "isd_kv_read_quant", "isd_admit", "isd_logprobs",
            "isd_test_preset_lora_counter", "isd_test_lora_work_item", "isd_test_verify_grid"]
 
 
@@ -57,6 +61,26 @@ class IsdLoraArgs(C.Structure):
         [(n, C.c_int32) for n in ("m", "n", "k", "rank")] + [("scale", C.c_float)]
 
 
+class IsdQuantLayerArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k_new", "v_new", "kv_pool", "attn_out", "attn_lse")]
+
+
+class IsdKvQuantArgs(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_row_stride", C.c_int64), ("v_row_stride", C.c_int64),
+                ("slot_map", C.c_void_p), ("kv_pool", C.c_void_p), ("n_tokens", C.c_int64)]
+
+
+class IsdAdmitArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("slots", "lens", "anchors", "result", "cu_len", "slot_map", "tok_req", "tok_pos")] + \
+        [("map_cap", C.c_int64), ("n", C.c_int32)]
+
+
+class IsdLogprobsArgs(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("logits_rows", C.c_int64), ("rows", C.c_void_p), ("tokens", C.c_void_p),
+                ("n", C.c_int32), ("top_n", C.c_int32)] + \
+        [(n, C.c_void_p) for n in ("logprob", "entropy", "top_id", "top_logprob")]
+
+
 _lib = None
 
 
@@ -89,6 +113,17 @@ def load():
         lib.isd_set_step_counter.restype = C.c_int
         lib.isd_lora_linear.argtypes = [vp, C.POINTER(IsdLoraArgs), vp]
         lib.isd_lora_linear.restype = C.c_int
+        lib.isd_attn_quant.argtypes = [vp, C.POINTER(IsdBatchState)] + [vp] * 7
+        lib.isd_attn_quant.restype = C.c_int
+        lib.isd_step_quant.argtypes = [vp, C.POINTER(IsdBatchState), C.POINTER(IsdQuantLayerArgs), C.c_int32, vp, vp,
+                                       C.POINTER(IsdVerifyOut), C.c_uint64, vp]
+        lib.isd_step_quant.restype = C.c_int
+        for n, t in (("isd_kv_write_quant", IsdKvQuantArgs), ("isd_kv_read_quant", IsdKvQuantArgs),
+                     ("isd_logprobs", IsdLogprobsArgs)):
+            getattr(lib, n).argtypes = [vp, C.POINTER(t), vp]
+            getattr(lib, n).restype = C.c_int
+        lib.isd_admit.argtypes = [vp, C.POINTER(IsdBatchState), C.POINTER(IsdAdmitArgs), vp]
+        lib.isd_admit.restype = C.c_int
         lib.isd_set_wait_limit.argtypes = [vp, C.c_uint32]
         lib.isd_set_wait_limit.restype = C.c_int
         lib.isd_test_preset_lora_counter.argtypes = [vp, C.c_int32, C.c_uint32, vp]
@@ -144,6 +179,28 @@ def _ptr(t):
     return t.data_ptr() if t.numel() > 0 else None
 
 
+def _arg(t, name, dtype, shape, device):
+    """Device pointer of a dense tensor argument that has to have this dtype and shape; None passes as NULL."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) \
+            or not t.is_contiguous():
+        got = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise IsdError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {got}")
+    return t.data_ptr() if t.numel() > 0 else None
+
+
+def _rows_arg(t, name, rows, heads, device):
+    """(device pointer, row stride in elements) of bf16 rows [rows, heads, 128] that are dense within a row."""
+    if t.device != device or t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, heads, 128):
+        raise IsdError(f"{name}: expected a bf16 tensor of shape {(rows, heads, 128)} on {device}, "
+                       f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    stride = heads * 128 if rows <= 1 else t.stride(0)
+    if rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128) or stride < heads * 128 or stride % 8):
+        raise IsdError(f"{name}: rows have to be dense and a multiple of 8 elements apart, got strides {t.stride()}")
+    return (t.data_ptr() if rows else None), stride
+
+
 def _stream():
     return torch.cuda.current_stream().cuda_stream
 
@@ -157,6 +214,24 @@ def alloc_verify_out(B: int, N: int, device) -> dict:
         accept_len=torch.zeros(B, **i32), n_emit=torch.zeros(B, **i32), repl_tok=torch.zeros(B, **i32),
         out_tok=torch.zeros(B, N, **i32), new_prop_tok=torch.zeros(B, NP, **i32),
         new_q_stats=torch.zeros(B, NP, 2, dtype=torch.float32, device=device))
+
+
+def alloc_kv_pool_quant(num_pages: int, n_kv_heads: int, device) -> torch.Tensor:
+    """A 4-bit cache of `num_pages` pages, empty (layout: include/isd.h)."""
+    return torch.zeros(num_pages, n_kv_heads, QUANT_TILE_BYTES, dtype=torch.uint8, device=device)
+
+
+def alloc_admit_maps(n: int, map_cap: int, device) -> dict:
+    i32 = dict(dtype=torch.int32, device=device)
+    return dict(result=torch.zeros(n, **i32), cu_len=torch.zeros(n + 1, **i32),
+                slot_map=torch.full((map_cap,), -1, dtype=torch.int64, device=device),
+                tok_req=torch.full((map_cap,), -1, **i32), tok_pos=torch.full((map_cap,), -1, **i32))
+
+
+def alloc_logprobs_out(n: int, top_n: int, device) -> dict:
+    f32 = dict(dtype=torch.float32, device=device)
+    return dict(logprob=torch.zeros(n, **f32), entropy=torch.zeros(n, **f32),
+                top_id=torch.zeros(n, top_n, dtype=torch.int32, device=device), top_logprob=torch.zeros(n, top_n, **f32))
 
 
 def isd_verify_static(cfg: IsdConfig, st: dict, logits_cur, q_prev_logits, step: int, out: dict):
@@ -176,6 +251,7 @@ class Isd:
         if not torch.cuda.is_available():
             raise IsdError("a CUDA device is required (there is no CPU path)")
         self.lib = load()
+        self.device = torch.device("cuda", torch.cuda.current_device())
         ld = {"f32": 0, "bf16": 1, torch.float32: 0, torch.bfloat16: 1, 0: 0, 1: 1}[logits_dtype]
         self.cfg = IsdConfig(batch, stride, n_q_heads, n_kv_heads, head_dim, page_size, vocab,
                              max_pages_per_slot, num_pages, ld, q_mode, propose_mode,
@@ -253,6 +329,86 @@ class Isd:
         args = IsdLoraArgs(_ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(gate), _ptr(t), _ptr(y), m, n, k, rank, scale)
         _check(self.lib.isd_lora_linear(self.ctx, C.byref(args), _stream()), "isd_lora_linear")
         return y
+
+    def _quant_ptrs(self, q, k_new, v_new, kv_pool, attn_out, attn_lse):
+        c, bf, Q = self.cfg, torch.bfloat16, 2 * self.N - 1
+        row, kv = (self.B, Q, c.n_q_heads, 128), (self.B, Q, c.n_kv_heads, 128)
+        return [_arg(q, "q", bf, row, self.device), _arg(k_new, "k_new", bf, kv, self.device),
+                _arg(v_new, "v_new", bf, kv, self.device), self._pool_ptr(kv_pool),
+                _arg(attn_out, "attn_out", bf, row, self.device), _arg(attn_lse, "attn_lse", torch.float32, row[:3], self.device)]
+
+    def _pool_ptr(self, kv_pool):
+        return _arg(kv_pool, "kv_pool", torch.uint8, (self.cfg.num_pages, self.cfg.n_kv_heads, QUANT_TILE_BYTES), self.device)
+
+    def isd_attn_quant(self, st, q, k_new, v_new, kv_pool, attn_out, attn_lse=None):
+        """isd_attn over the 4-bit cache `kv_pool` (uint8 [num_pages, Hkv, 2176], see alloc_kv_pool_quant)."""
+        p = self._quant_ptrs(q, k_new, v_new, kv_pool, attn_out, attn_lse)
+        s = self.state_struct(st)
+        _check(self.lib.isd_attn_quant(self.ctx, C.byref(s), *p, _stream()), "isd_attn_quant")
+
+    def quant_layer_args(self, layers):
+        """Host array of isd_quant_layer_args from dicts with q, k_new, v_new, kv_pool, attn_out[, attn_lse]."""
+        arr = (IsdQuantLayerArgs * len(layers))()
+        for i, a in enumerate(layers):
+            arr[i] = IsdQuantLayerArgs(*self._quant_ptrs(a["q"], a["k_new"], a["v_new"], a["kv_pool"], a["attn_out"],
+                                                         a.get("attn_lse")))
+        return arr
+
+    def isd_step_quant(self, st, layers, logits_cur, q_prev_logits, out, step: int, st_struct: IsdBatchState | None = None):
+        """isd_step_layers on 4-bit caches; `layers`: what quant_layer_args returned."""
+        s = st_struct if st_struct is not None else self.state_struct(st)
+        o = self.out_struct(out)
+        _check(self.lib.isd_step_quant(self.ctx, C.byref(s), layers, len(layers), _ptr(logits_cur), _ptr(q_prev_logits),
+                                       C.byref(o), step, _stream()), "isd_step_quant")
+
+    def _kv_quant_args(self, k, v, slot_map, kv_pool):
+        n, h = slot_map.numel(), self.cfg.n_kv_heads
+        (kp, ks), (vp, vs) = _rows_arg(k, "k", n, h, self.device), _rows_arg(v, "v", n, h, self.device)
+        return IsdKvQuantArgs(kp, vp, ks, vs, _arg(slot_map, "slot_map", torch.int64, (n,), self.device),
+                              self._pool_ptr(kv_pool), n)
+
+    def isd_kv_write_quant(self, k, v, slot_map, kv_pool):
+        """Quantise rows k, v [T, Hkv, 128] bf16 (rows may be strided) into the slots of slot_map [T] int64 (< 0: skipped)."""
+        a = self._kv_quant_args(k, v, slot_map, kv_pool)
+        _check(self.lib.isd_kv_write_quant(self.ctx, C.byref(a), _stream()), "isd_kv_write_quant")
+
+    def isd_kv_read_quant(self, kv_pool, slot_map, k, v):
+        """The values of the slots of slot_map as bf16 into k, v [T, Hkv, 128] (rows may be strided)."""
+        a = self._kv_quant_args(k, v, slot_map, kv_pool)
+        _check(self.lib.isd_kv_read_quant(self.ctx, C.byref(a), _stream()), "isd_kv_read_quant")
+
+    def isd_admit(self, st, slots, lens, anchors, maps):
+        """Admit requests (slot, cached length, anchor token: int32 [n]) into inactive slots; `maps`: see alloc_admit_maps
+        (slot_map, tok_req, tok_pos may be None)."""
+        n, i32, dev = slots.numel(), torch.int32, self.device
+        some = next((maps[k] for k in ("slot_map", "tok_req", "tok_pos") if maps.get(k) is not None), None)
+        cap = 0x7FFFFFFF if some is None else some.numel()
+        a = IsdAdmitArgs(_arg(slots, "slots", i32, (n,), dev), _arg(lens, "lens", i32, (n,), dev),
+                         _arg(anchors, "anchors", i32, (n,), dev), _arg(maps["result"], "result", i32, (n,), dev),
+                         _arg(maps["cu_len"], "cu_len", i32, (n + 1,), dev),
+                         _arg(maps.get("slot_map"), "slot_map", torch.int64, (cap,), dev),
+                         _arg(maps.get("tok_req"), "tok_req", i32, (cap,), dev),
+                         _arg(maps.get("tok_pos"), "tok_pos", i32, (cap,), dev), cap, n)
+        s = self.state_struct(st)
+        _check(self.lib.isd_admit(self.ctx, C.byref(s), C.byref(a), _stream()), "isd_admit")
+
+    def isd_logprobs(self, logits, tokens, rows=None, top_n: int = 0, out=None) -> dict:
+        """Log probability of tokens [n] int32 (< 0: skipped) under the rows of `logits` (flattened to [*, V]; `rows` [n]
+        int32 picks them, None: row i), entropy and the top_n alternatives.  Allocates `out` when not given."""
+        n, V = tokens.numel(), self.cfg.vocab
+        dt = torch.bfloat16 if self.cfg.logits_dtype == 1 else torch.float32
+        total = logits.numel() // V
+        if rows is None and n > total:
+            raise IsdError(f"logits: {total} rows for {n} tokens")
+        out = alloc_logprobs_out(n, top_n, self.device) if out is None else out
+        i32, f32, dev = torch.int32, torch.float32, self.device
+        a = IsdLogprobsArgs(_arg(logits, "logits", dt, (*logits.shape[:-1], V), dev), total, _arg(rows, "rows", i32, (n,), dev),
+                            _arg(tokens, "tokens", i32, (n,), dev), n, top_n, _arg(out["logprob"], "logprob", f32, (n,), dev),
+                            _arg(out.get("entropy"), "entropy", f32, (n,), dev),
+                            _arg(out["top_id"], "top_id", i32, (n, top_n), dev) if top_n else None,
+                            _arg(out["top_logprob"], "top_logprob", f32, (n, top_n), dev) if top_n else None)
+        _check(self.lib.isd_logprobs(self.ctx, C.byref(a), _stream()), "isd_logprobs")
+        return out
 
     def isd_set_step_counter(self, counter):
         """`counter`: a CUDA uint32 / int32 tensor of one element, or None."""

@@ -1,0 +1,155 @@
+// isd_admit: requests enter free slots (Sec. 3.3 (2): the stationary batch takes new requests without the host).
+// Pages come from the free stack in request order, by an exclusive prefix sum of what the requests ask for, so the
+// result does not depend on thread scheduling.  Two kernels: a CTA that plans and commits the state, and a grid that
+// writes the tokens' maps.
+#include <limits.h>
+
+#include "isd_commit.cuh"
+
+namespace {
+
+struct AdmitParams {
+  int B, Q, max_pages, mask_token, n;
+  int64_t map_cap;
+  const int32_t* slots;
+  const int32_t* lens;
+  const int32_t* anchors;
+  int32_t* result;
+  int32_t* cu_len;
+  int64_t* slot_map;
+  int32_t* tok_req;
+  int32_t* tok_pos;
+  int32_t* ctx_len;
+  int32_t* n_ver;
+  int32_t* block_tok;
+  int32_t* q_row0;
+  int32_t* page_table;
+  const int32_t* free_stack;
+  int32_t* free_top;
+  uint8_t* active;
+  uint32_t* slot_status;
+  int* mark;
+};
+
+constexpr int kAdmitThreads = 1024;
+
+__global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitParams P) {
+  __shared__ int sm_warp[33];
+  pdl_wait();
+  pdl_launch_dependents();
+  // the first request of a slot counts
+  for (int i = threadIdx.x; i < P.n; i += kAdmitThreads) {
+    const int b = P.slots[i];
+    if (b >= 0 && b < P.B) atomicMin(P.mark + b, i);
+  }
+  __syncthreads();
+  const int top = *P.free_top;
+  int64_t pages0 = 0, toks0 = 0;  // asked for by valid requests of earlier rounds
+  int served_pages = 0, served_toks = 0;
+  for (int base = 0; base < P.n; base += kAdmitThreads) {
+    const int i = base + threadIdx.x;
+    uint32_t why = 0;
+    int b = -1, len = 0, want = 0;
+    if (i < P.n) {
+      b = P.slots[i];
+      len = P.lens[i];
+      if (b < 0 || b >= P.B || P.active[b] || __ldcg(P.mark + b) != i) {
+        why = ISD_ST_BAD_SLOT;
+      } else if (len < 0 || len > (long long)P.max_pages * ISD_PAGE - P.Q) {
+        why = ISD_ST_SLOT_CAPACITY;
+      } else {
+        want = (len + P.Q + ISD_PAGE - 1) / ISD_PAGE;
+      }
+    }
+    const bool asks = i < P.n && !why;
+    // (a round asks for at most 1024 requests; sums in 64 bits over the two halves of a length)
+    int tp, tl, th;
+    const int64_t before_p = pages0 + block_exclusive_scan(asks ? want : 0, sm_warp, tp);
+    const int lo = asks ? (len & 0xFFFF) : 0, hi = asks ? (len >> 16) : 0;
+    const int64_t sl = block_exclusive_scan(lo, sm_warp, tl), sh = block_exclusive_scan(hi, sm_warp, th);
+    const int64_t before_t = toks0 + sl + (sh << 16);
+    pages0 += tp;
+    toks0 += tl + ((int64_t)th << 16);
+    if (asks) {
+      if (before_p + want > top) why = ISD_ST_POOL_EXHAUSTED;
+      else if (before_t + len > P.map_cap) why = ISD_ST_MAP_FULL;
+    }
+    const bool ok = asks && !why;
+    int n_p, n_t;
+    block_exclusive_scan(ok ? want : 0, sm_warp, n_p);
+    const int my_t = block_exclusive_scan(ok ? len : 0, sm_warp, n_t);
+    if (i < P.n) {
+      P.result[i] = (int32_t)why;
+      P.cu_len[i] = served_toks + my_t;
+    }
+    served_toks += n_t;
+    served_pages += n_p;
+    if (ok) {
+      P.ctx_len[b] = len;
+      P.n_ver[b] = 0;
+      P.q_row0[b] = 0;
+      P.slot_status[b] = 0;
+      P.active[b] = 1;
+      for (int m = 0; m < P.Q; ++m) P.block_tok[(size_t)b * P.Q + m] = m == 0 ? P.anchors[i] : P.mask_token;
+      for (int j = 0; j < want; ++j) P.page_table[(size_t)b * P.max_pages + j] = P.free_stack[top - 1 - (before_p + j)];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < P.n; i += kAdmitThreads) {
+    const int b = P.slots[i];
+    if (b >= 0 && b < P.B) P.mark[b] = INT_MAX;
+  }
+  if (threadIdx.x == 0) {
+    P.cu_len[P.n] = served_toks;
+    *P.free_top = top - served_pages;
+  }
+}
+
+__global__ void __launch_bounds__(256) admit_maps_kernel(const AdmitParams P) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int total = P.cu_len[P.n];
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+    // last request whose tokens begin at or before t (requests without tokens share their successor's beginning)
+    int lo = 0, hi = P.n;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (P.cu_len[mid + 1] > t) hi = mid; else lo = mid + 1;
+    }
+    const int pos = (int)t - P.cu_len[lo];
+    if (P.slot_map)
+      P.slot_map[t] = (int64_t)P.page_table[(size_t)P.slots[lo] * P.max_pages + pos / ISD_PAGE] * ISD_PAGE + pos % ISD_PAGE;
+    if (P.tok_req) P.tok_req[t] = lo;
+    if (P.tok_pos) P.tok_pos[t] = pos;
+  }
+}
+
+}  // namespace
+
+int isd_admit_create(isd_ctx* ctx) {
+  const size_t B = (size_t)ctx->cfg.batch;
+  if (cudaMalloc(&ctx->admit_mark, sizeof(int) * B) != cudaSuccess) return ISD_ERR_NO_MEMORY;
+  return cudaMemset(ctx->admit_mark, 0x7F, sizeof(int) * B) == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
+}
+
+void isd_admit_destroy(isd_ctx* ctx) { cudaFree(ctx->admit_mark); }
+
+int isd_launch_admit(isd_ctx* ctx, isd_batch_state* st, const isd_admit_args* a, cudaStream_t stream) {
+  const isd_config& c = ctx->cfg;
+  AdmitParams P;
+  P.B = c.batch; P.Q = ctx->Q; P.max_pages = c.max_pages_per_slot; P.mask_token = c.mask_token_id; P.n = a->n; P.map_cap = a->map_cap;
+  P.slots = a->slots; P.lens = a->lens; P.anchors = a->anchors; P.result = a->result; P.cu_len = a->cu_len;
+  P.slot_map = a->slot_map; P.tok_req = a->tok_req; P.tok_pos = a->tok_pos;
+  P.ctx_len = st->ctx_len; P.n_ver = st->n_ver; P.block_tok = st->block_tok; P.q_row0 = st->q_row0; P.page_table = st->page_table;
+  P.free_stack = st->free_stack; P.free_top = st->free_top; P.active = st->active; P.slot_status = st->slot_status;
+  P.mark = ctx->admit_mark;
+  cudaError_t e = isd_launch_pdl(admit_plan_kernel, dim3(1), dim3(kAdmitThreads), 0, stream, P);
+  ctx->launches++;
+  if (e == cudaSuccess && a->n > 0 && a->map_cap > 0 && (a->slot_map || a->tok_req || a->tok_pos)) {
+    const int64_t ctas = (a->map_cap + 255) / 256;
+    const int most = ctx->num_sms * 8;
+    e = isd_launch_pdl(admit_maps_kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, stream, P);
+    ctx->launches++;
+  }
+  return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
+}

@@ -31,6 +31,12 @@ int check_state(const isd_batch_state* st) {
   return ISD_OK;
 }
 
+// The context's scratch and the stream's work belong to the device the context was created on.
+bool on_device(const isd_ctx* ctx) {
+  int dev = -1;
+  return ctx && cudaGetDevice(&dev) == cudaSuccess && dev == ctx->device;
+}
+
 int check_out(const isd_ctx* ctx, const isd_verify_out* o) {
   if (!o) return ISD_ERR_INVALID_ARG;
   if (!o->accept_len || !o->n_emit || !o->repl_tok || !o->out_tok) return ISD_ERR_INVALID_ARG;
@@ -95,6 +101,9 @@ int isd_create(const isd_config* cfg, isd_ctx** out) {
   if (rc == ISD_OK && c.top_k > 0) rc = isd_verify_topk_create(ctx);
   if (rc == ISD_OK) rc = isd_lora_create(ctx);
   if (rc == ISD_OK) rc = isd_attn_tc_create(ctx);
+  if (rc == ISD_OK) rc = isd_attn_quant_create(ctx);
+  if (rc == ISD_OK) rc = isd_admit_create(ctx);
+  if (rc == ISD_OK) rc = isd_logprobs_create(ctx);
   if (rc == ISD_OK && cudaDeviceSynchronize() != cudaSuccess) rc = ISD_ERR_CUDA;
   if (rc != ISD_OK) {
     isd_destroy(ctx);
@@ -108,6 +117,9 @@ int isd_destroy(isd_ctx* ctx) {
   if (!ctx) return ISD_ERR_INVALID_ARG;
   cudaDeviceSynchronize();
   isd_attn_tc_destroy(ctx);
+  isd_attn_quant_destroy(ctx);
+  isd_admit_destroy(ctx);
+  isd_logprobs_destroy(ctx);
   isd_verify_topk_destroy(ctx);
   isd_lora_destroy(ctx);
   cudaFree(ctx->row_part);
@@ -199,6 +211,74 @@ int isd_step_layers(isd_ctx* ctx, isd_batch_state* st, const isd_layer_args* lay
     if (rc != ISD_OK) return rc;
   }
   return verify_then_commit(ctx, st, logits_cur, q_prev_logits, step, out, cuda_stream);
+}
+
+int isd_attn_quant(isd_ctx* ctx, const isd_batch_state* st, const void* q, const void* k_new, const void* v_new,
+                   void* kv_pool, void* attn_out, float* attn_lse, void* cuda_stream) {
+  if (!on_device(ctx)) return ISD_ERR_INVALID_ARG;
+  int rc = check_state(st);
+  if (rc != ISD_OK) return rc;
+  if (!q || !k_new || !v_new || !kv_pool || !attn_out) return ISD_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(kv_pool) || !aligned16(attn_out))
+    return ISD_ERR_ALIGNMENT;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  rc = isd_launch_kv_append_quant(ctx, st, k_new, v_new, kv_pool, s);
+  if (rc != ISD_OK) return rc;
+  return isd_launch_attn_quant(ctx, st, q, k_new, v_new, kv_pool, attn_out, attn_lse, s);
+}
+
+int isd_step_quant(isd_ctx* ctx, isd_batch_state* st, const isd_quant_layer_args* layers, int32_t n_layers,
+                   const void* logits_cur, const void* q_prev_logits, const isd_verify_out* out, uint64_t step,
+                   void* cuda_stream) {
+  if (!ctx || !layers || n_layers < 1 || !out) return ISD_ERR_INVALID_ARG;
+  for (int32_t l = 0; l < n_layers; ++l) {
+    const isd_quant_layer_args& a = layers[l];
+    const int rc = isd_attn_quant(ctx, st, a.q, a.k_new, a.v_new, a.kv_pool, a.attn_out, a.attn_lse, cuda_stream);
+    if (rc != ISD_OK) return rc;
+  }
+  return verify_then_commit(ctx, st, logits_cur, q_prev_logits, step, out, cuda_stream);
+}
+
+static int check_kv_quant(const isd_ctx* ctx, const isd_kv_quant_args* a) {
+  if (!on_device(ctx) || !a || a->n_tokens < 0) return ISD_ERR_INVALID_ARG;
+  if (a->n_tokens == 0) return ISD_OK;
+  if (!a->k || !a->v || !a->slot_map || !a->kv_pool) return ISD_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)ctx->cfg.n_kv_heads * ISD_HEAD_DIM;
+  if (a->k_row_stride < row || a->v_row_stride < row || a->k_row_stride % 8 != 0 || a->v_row_stride % 8 != 0)
+    return ISD_ERR_INVALID_ARG;
+  if (a->n_tokens > (int64_t)0x7FFFFFFF * 16 / ctx->cfg.n_kv_heads) return ISD_ERR_INVALID_ARG;
+  if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->kv_pool)) return ISD_ERR_ALIGNMENT;
+  return ISD_OK;
+}
+
+int isd_kv_write_quant(isd_ctx* ctx, const isd_kv_quant_args* a, void* cuda_stream) {
+  const int rc = check_kv_quant(ctx, a);
+  if (rc != ISD_OK || a->n_tokens == 0) return rc;
+  return isd_launch_kv_write_quant(ctx, a, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+int isd_kv_read_quant(isd_ctx* ctx, const isd_kv_quant_args* a, void* cuda_stream) {
+  const int rc = check_kv_quant(ctx, a);
+  if (rc != ISD_OK || a->n_tokens == 0) return rc;
+  return isd_launch_kv_read_quant(ctx, a, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+int isd_admit(isd_ctx* ctx, isd_batch_state* st, const isd_admit_args* a, void* cuda_stream) {
+  if (!on_device(ctx) || !a) return ISD_ERR_INVALID_ARG;
+  const int rc = check_state(st);
+  if (rc != ISD_OK) return rc;
+  if (a->n < 0 || a->map_cap < 0 || a->map_cap > 0x7FFFFFFF || !a->cu_len) return ISD_ERR_INVALID_ARG;
+  if (a->n > 0 && (!a->slots || !a->lens || !a->anchors || !a->result)) return ISD_ERR_INVALID_ARG;
+  return isd_launch_admit(ctx, st, a, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+int isd_logprobs(isd_ctx* ctx, const isd_logprobs_args* a, void* cuda_stream) {
+  if (!on_device(ctx) || !a || a->n < 0 || a->logits_rows < 0) return ISD_ERR_INVALID_ARG;
+  if (a->top_n < 0 || a->top_n > ISD_MAX_TOP_LOGPROBS || a->top_n > ctx->cfg.vocab) return ISD_ERR_INVALID_ARG;
+  if (a->n == 0) return ISD_OK;
+  if (!a->logits || !a->tokens || !a->logprob || (a->top_n > 0 && (!a->top_id || !a->top_logprob))) return ISD_ERR_INVALID_ARG;
+  if (!aligned16(a->logits)) return ISD_ERR_ALIGNMENT;
+  return isd_launch_logprobs(ctx, a, reinterpret_cast<cudaStream_t>(cuda_stream));
 }
 
 int isd_lora_linear(isd_ctx* ctx, const isd_lora_args* a, void* cuda_stream) {

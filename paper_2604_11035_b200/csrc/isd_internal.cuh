@@ -75,6 +75,11 @@ struct isd_ctx {
   uint32_t* step_counter;
   // ---- isd_step: arrivals of the last verification kernel's CTAs (the last one commits), zero between calls
   int* step_ticket;
+  // ---- isd_admit
+  int* admit_mark;       // [B] first request that names the slot (above every index between calls)
+  // ---- isd_logprobs: partial results of rows cut into pieces, arrivals per row (zero between calls)
+  void* lp_part;
+  int* lp_ticket;
   // ---- time limit of every device-side wait, nanoseconds
   unsigned long long wait_ns;
   // ---- status
@@ -361,4 +366,18 @@ int isd_launch_kv_append(isd_ctx* ctx, const isd_batch_state* st, const void* k_
 int isd_launch_attn_tc(isd_ctx* ctx, const isd_batch_state* st, const void* q, const void* k_new,
                        const void* v_new, void* k_pool, void* v_pool, void* out, float* lse,
                        cudaStream_t stream);
+int isd_attn_quant_create(isd_ctx* ctx);
+void isd_attn_quant_destroy(isd_ctx* ctx);
+int isd_launch_attn_quant(isd_ctx* ctx, const isd_batch_state* st, const void* q, const void* k_new, const void* v_new,
+                          void* kv_pool, void* out, float* lse, cudaStream_t stream);
+int isd_launch_kv_append_quant(isd_ctx* ctx, const isd_batch_state* st, const void* k_new, const void* v_new,
+                               void* kv_pool, cudaStream_t stream);
+int isd_launch_kv_write_quant(isd_ctx* ctx, const isd_kv_quant_args* a, cudaStream_t stream);
+int isd_launch_kv_read_quant(isd_ctx* ctx, const isd_kv_quant_args* a, cudaStream_t stream);
+int isd_admit_create(isd_ctx* ctx);
+void isd_admit_destroy(isd_ctx* ctx);
+int isd_launch_admit(isd_ctx* ctx, isd_batch_state* st, const isd_admit_args* a, cudaStream_t stream);
+int isd_logprobs_create(isd_ctx* ctx);
+void isd_logprobs_destroy(isd_ctx* ctx);
+int isd_launch_logprobs(isd_ctx* ctx, const isd_logprobs_args* a, cudaStream_t stream);
 int isd_attn_tc_scratch_bytes(const isd_ctx* ctx, size_t* part_o, size_t* part_ml);

@@ -1,0 +1,214 @@
+// The 4-bit KV cache's traffic: the block append of isd_attn_quant, isd_kv_write_quant and isd_kv_read_quant
+// (Sec. 3.3 (2): KV rows enter the paged cache by one batched scatter).
+//
+// All three work on runs of consecutive tokens inside a page, one warp per (run, kv head): a V word holds eight
+// tokens of a dim, so a run's words are built in registers and stored whole.
+#include "isd_quant.cuh"
+
+namespace {
+
+struct AppendParams {
+  int B, Q, N, Hkv, max_pages, num_pages;
+  const int32_t* ctx_len;
+  const int32_t* n_ver;
+  const uint8_t* active;
+  const int32_t* page_table;
+  uint32_t* slot_status;
+  uint32_t* global_status;
+  const __nv_bfloat16* k_new;
+  const __nv_bfloat16* v_new;
+  uint8_t* pool;
+};
+
+constexpr int kAppendWarps = 3;  // a block of up to 31 rows lies in at most three pages
+
+// One CTA per (slot, kv head): validate the slot's page-table prefix, then a warp per page of the block.
+__global__ void __launch_bounds__(kAppendWarps * 32) kv_append_quant_kernel(const AppendParams P) {
+  const int b = blockIdx.x, g = blockIdx.y;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (!P.active[b]) return;
+  const int nv = P.n_ver[b];
+  if (nv < 0 || nv > P.N - 1) return;
+  const int ql = nv + P.N, ctx = P.ctx_len[b];
+  // (a length near 2^31 must not wrap: compare before adding)
+  if (ctx < 0 || ctx > (long long)P.max_pages * ISD_PAGE - ql) {
+    if (threadIdx.x == 0 && g == 0) {
+      atomicOr(&P.slot_status[b], ISD_ST_SLOT_CAPACITY);
+      atomicOr(P.global_status, ISD_ST_SLOT_CAPACITY);
+    }
+    return;
+  }
+  const int pages = (ctx + ql + ISD_PAGE - 1) / ISD_PAGE;
+  const int32_t* pt = P.page_table + (size_t)b * P.max_pages;
+  int bad = 0;
+  for (int pg = threadIdx.x; pg < pages; pg += blockDim.x) {
+    const int id = pt[pg];
+    bad |= id < 0 || id >= P.num_pages;
+  }
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0 && g == 0) {
+      atomicOr(&P.slot_status[b], ISD_ST_BAD_PAGE_ID);
+      atomicOr(P.global_status, ISD_ST_BAD_PAGE_ID);
+    }
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int pg = ctx / ISD_PAGE + warp;
+  if (pg >= pages) return;
+  const int off = warp == 0 ? ctx % ISD_PAGE : 0;
+  const int row0 = warp == 0 ? 0 : warp * ISD_PAGE - ctx % ISD_PAGE;
+  const int cnt = min(ISD_PAGE - off, ql - row0);
+  uint8_t* tile = P.pool + ((size_t)pt[pg] * P.Hkv + g) * kQTile;
+  const size_t stride = (size_t)P.Hkv * ISD_HEAD_DIM;
+  const size_t src = ((size_t)b * P.Q + row0) * stride + (size_t)g * ISD_HEAD_DIM;
+  quant_store_run<false>(P.k_new + src, stride, P.v_new + src, stride, tile, off, cnt);
+  // Tokens behind the block are emptied: their probability is zero, but the tensor cores multiply it by code minus zero,
+  // which needs a finite zero.
+  if (pg == pages - 1) {
+    uint16_t* meta = reinterpret_cast<uint16_t*>(tile + kQOffMeta);
+    for (int i = lane; i < 64; i += 32)
+      if ((i & 15) >= off + cnt) meta[i] = (i & 16) ? kQZeroOne : (uint16_t)0;
+  }
+}
+
+struct RowsParams {
+  __nv_bfloat16* k;
+  __nv_bfloat16* v;
+  size_t k_stride, v_stride;
+  const int64_t* slot_map;
+  uint8_t* pool;
+  int64_t n_tokens, n_slots;
+  int Hkv;
+  uint32_t* global_status;
+};
+
+constexpr int kWindow = 16;  // tokens whose runs one warp owns
+constexpr int kRowsWarps = 4;
+
+// The runs (consecutive slots of one page at consecutive tokens) that start in a window of kWindow tokens, one warp per
+// (window, kv head): a run belongs to the window of its first token and may reach up to 15 tokens into the next one, so
+// that no page of a request is cut between two warps, wherever the window's border falls.
+template <class Body>
+__device__ __forceinline__ void for_runs(const RowsParams& P, Body body) {
+  const int lane = threadIdx.x & 31;
+  const int64_t item = (int64_t)blockIdx.x * kRowsWarps + (threadIdx.x >> 5);
+  const int g = (int)(item % P.Hkv);
+  const int64_t t0 = item / P.Hkv * kWindow;
+  if (t0 >= P.n_tokens) return;
+  const int64_t t = t0 + lane;
+  int64_t slot = t < P.n_tokens ? P.slot_map[t] : -1;
+  int64_t prev = __shfl_up_sync(0xffffffffu, slot, 1);
+  if (lane == 0) prev = t0 > 0 ? P.slot_map[t0 - 1] : -1;
+  if (slot >= P.n_slots) {
+    if (g == 0 && lane < kWindow) atomicOr(P.global_status, ISD_ST_BAD_PAGE_ID);
+    slot = -1;
+  }
+  // a token goes on the run before it unless it is the first of a page (prev + 1 == slot >= 1 then implies prev valid)
+  const bool goes_on = slot >= 0 && (slot & 15) != 0 && prev == slot - 1;
+  const uint32_t on = __ballot_sync(0xffffffffu, goes_on);
+  uint32_t heads = __ballot_sync(0xffffffffu, slot >= 0 && !goes_on && lane < kWindow);
+  while (heads) {
+    const int l = __ffs(heads) - 1;
+    heads &= heads - 1;
+    const uint32_t after = l < 31 ? ~(on >> (l + 1)) : 1u;  // first token after the head that does not go on
+    const int cnt = min(__ffs(after), 32 - l);
+    const int64_t s = __shfl_sync(0xffffffffu, slot, l);
+    body(t0 + l, (int)(s & 15), cnt, P.pool + ((size_t)(s >> 4) * P.Hkv + g) * kQTile, g);
+  }
+}
+
+__global__ void __launch_bounds__(kRowsWarps * 32) kv_write_quant_kernel(const RowsParams P) {
+  pdl_wait();
+  pdl_launch_dependents();
+  for_runs(P, [&](int64_t t, int off, int cnt, uint8_t* tile, int g) {
+    quant_store_run<true>(P.k + (size_t)t * P.k_stride + g * ISD_HEAD_DIM, P.k_stride,
+                          P.v + (size_t)t * P.v_stride + g * ISD_HEAD_DIM, P.v_stride, tile, off, cnt);
+  });
+}
+
+// bf16 pair of scale * (code - zero): the integer difference and its product with the scale are exact in fp32
+__device__ __forceinline__ uint32_t value_pair(uint32_t d, float s0, float s1) {
+  const float lo = __uint_as_float(d << 16) * s0, hi = __uint_as_float(d & 0xFFFF0000u) * s1;
+  return as_u32(__floats2bfloat162_rn(lo, hi));
+}
+
+__global__ void __launch_bounds__(kRowsWarps * 32) kv_read_quant_kernel(const RowsParams P) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, hl = lane & 15, par = lane >> 4;
+  for_runs(P, [&](int64_t t0, int off, int cnt, const uint8_t* tile, int g) {
+    const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + kQOffMeta);
+    __nv_bfloat16* k = P.k + (size_t)t0 * P.k_stride + g * ISD_HEAD_DIM;
+    __nv_bfloat16* v = P.v + (size_t)t0 * P.v_stride + g * ISD_HEAD_DIM;
+    // K: half-warp per token, eight dims a lane
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = 2 * i + par;
+      if (t < off || t >= off + cnt) continue;
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + (hl >> 2) * 256 + t * 16 + (hl & 3) * 4);
+      const float s = bf16_bits_to_f32(meta[t]);
+      const uint32_t z = meta[16 + t] * 0x10001u;
+      uint4 o;
+      o.x = value_pair(sub_zero(codes_to_bf16(w), z), s, s);
+      o.y = value_pair(sub_zero(codes_to_bf16(w >> 4), z), s, s);
+      o.z = value_pair(sub_zero(codes_to_bf16(w >> 8), z), s, s);
+      o.w = value_pair(sub_zero(codes_to_bf16(w >> 12), z), s, s);
+      *reinterpret_cast<uint4*>(k + (size_t)(t - off) * P.k_stride + hl * 8) = o;
+    }
+    // V: four dims a lane, all tokens of the run
+    const uint4* src = reinterpret_cast<const uint4*>(tile + kQOffV + lane * 32);
+    const uint4 a = src[0], b = src[1];
+    const uint32_t w[2][4] = {{a.x, a.z, b.x, b.z}, {a.y, a.w, b.y, b.w}};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {  // token pair 2i, 2i + 1
+      const float s0 = bf16_bits_to_f32(meta[32 + 2 * i]), s1 = bf16_bits_to_f32(meta[32 + 2 * i + 1]);
+      const uint32_t z = *reinterpret_cast<const uint32_t*>(meta + 48 + 2 * i);
+      uint32_t p[4];
+#pragma unroll
+      for (int d = 0; d < 4; ++d) p[d] = value_pair(sub_zero(codes_to_bf16(w[i >> 2][d] >> (4 * (i & 3))), z), s0, s1);
+      const int t = 2 * i;
+      if (t >= off && t < off + cnt)
+        *reinterpret_cast<uint2*>(v + (size_t)(t - off) * P.v_stride + lane * 4) =
+            make_uint2(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[2], p[3], 0x5410));
+      if (t + 1 >= off && t + 1 < off + cnt)
+        *reinterpret_cast<uint2*>(v + (size_t)(t + 1 - off) * P.v_stride + lane * 4) =
+            make_uint2(__byte_perm(p[0], p[1], 0x7632), __byte_perm(p[2], p[3], 0x7632));
+    }
+  });
+}
+
+template <class Kernel>
+int launch_rows(isd_ctx* ctx, const isd_kv_quant_args* a, Kernel kernel, cudaStream_t stream) {
+  RowsParams P;
+  P.k = (__nv_bfloat16*)a->k; P.v = (__nv_bfloat16*)a->v;
+  P.k_stride = (size_t)a->k_row_stride; P.v_stride = (size_t)a->v_row_stride;
+  P.slot_map = a->slot_map; P.pool = (uint8_t*)a->kv_pool; P.n_tokens = a->n_tokens;
+  P.n_slots = (int64_t)ctx->cfg.num_pages * ISD_PAGE; P.Hkv = ctx->cfg.n_kv_heads; P.global_status = ctx->global_status;
+  const int64_t items = (a->n_tokens + kWindow - 1) / kWindow * P.Hkv;
+  const cudaError_t e = isd_launch_pdl(kernel, dim3((unsigned)((items + kRowsWarps - 1) / kRowsWarps)), dim3(kRowsWarps * 32), 0, stream, P);
+  ctx->launches++;
+  return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
+}
+
+}  // namespace
+
+int isd_launch_kv_append_quant(isd_ctx* ctx, const isd_batch_state* st, const void* k_new, const void* v_new,
+                               void* kv_pool, cudaStream_t stream) {
+  const isd_config& c = ctx->cfg;
+  AppendParams P;
+  P.B = c.batch; P.Q = ctx->Q; P.N = c.stride; P.Hkv = c.n_kv_heads; P.max_pages = c.max_pages_per_slot; P.num_pages = c.num_pages;
+  P.ctx_len = st->ctx_len; P.n_ver = st->n_ver; P.active = st->active; P.page_table = st->page_table;
+  P.slot_status = st->slot_status; P.global_status = ctx->global_status;
+  P.k_new = (const __nv_bfloat16*)k_new; P.v_new = (const __nv_bfloat16*)v_new; P.pool = (uint8_t*)kv_pool;
+  const cudaError_t e = isd_launch_pdl(kv_append_quant_kernel, dim3(c.batch, c.n_kv_heads), dim3(kAppendWarps * 32), 0, stream, P);
+  ctx->launches++;
+  return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
+}
+
+int isd_launch_kv_write_quant(isd_ctx* ctx, const isd_kv_quant_args* a, cudaStream_t stream) {
+  return launch_rows(ctx, a, kv_write_quant_kernel, stream);
+}
+int isd_launch_kv_read_quant(isd_ctx* ctx, const isd_kv_quant_args* a, cudaStream_t stream) {
+  return launch_rows(ctx, a, kv_read_quant_kernel, stream);
+}

@@ -1,0 +1,168 @@
+"""isd_logprobs against 64-bit log-softmax and a stable sort (needs a B200)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_11035_b200 as isd_pkg
+from paper_2604_11035_b200.binding import ST_BAD_TOKEN_ID, ST_NONFINITE_LOGIT
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def make(V, dtype, invt=1.0):
+    return isd_pkg.Isd(batch=1, stride=1, n_q_heads=8, n_kv_heads=8, vocab=V, max_pages_per_slot=4, num_pages=4, logits_dtype=dtype,
+                       inv_temperature=invt)
+
+
+def check(isd, logits, tokens, rows=None, top=0, invt=1.0, bad_rows=(), out=None):
+    """Runs and compares.  Bounds: an exponent's argument (l - max) * invT * log2 e of magnitude a is off by 3 * 2^-24 * a, its
+    exponential by two more ulp, so where the law has weight (a < 64) a term is off by 2^-16 at most, and below 2^-17 of itself for the terms that
+    matter (a < 32: 3 * 32 * 2^-24 + 2^-22 < 2^-17); a sum of V terms in chains of at most 2^10 additions adds 2^-14.  The log of the sum
+    is off by that; a log probability also by the rounding of (l - max) * invT: 2^-23 of it.  Entropy = log sum - sum w / sum, whose
+    two parts are bounded by log V and off by the same relative amounts."""
+    n, V = tokens.numel(), logits.shape[-1]
+    flat = logits.reshape(-1, V)
+    got = isd.isd_logprobs(logits, tokens, rows=rows, top_n=top, out=out)
+    g = {k: v.double().cpu().numpy() if v.dtype == torch.float32 else v.cpu().numpy() for k, v in got.items()}
+    idx = (rows if rows is not None else torch.arange(n, device=DEV)).long().cpu()
+    tok = tokens.long().cpu()
+    for i in range(n):
+        if tok[i] < 0 or tok[i] >= V or not 0 <= idx[i] < flat.shape[0] or int(idx[i]) in bad_rows:
+            assert np.isnan(g["logprob"][i]) and np.isnan(g["entropy"][i]), i
+            assert (g["top_id"][i] == -1).all() and np.isnan(g["top_logprob"][i]).all(), i
+            continue
+        row = flat[idx[i]].cpu()
+        lp = torch.log_softmax(row.double() * invt, 0).numpy()
+        p = np.exp(lp)
+        H = -(p[p > 0] * lp[p > 0]).sum()
+        tol = 2.0 ** -14 + 2.0 ** -17 + 2.0 ** -23 * np.abs(lp)
+        x = int(tok[i])
+        if np.isinf(lp[x]):
+            assert g["logprob"][i] == lp[x]
+        else:
+            assert abs(g["logprob"][i] - lp[x]) <= tol[x], (i, g["logprob"][i], lp[x])
+        assert abs(g["entropy"][i] - H) <= (2.0 ** -14 + 2.0 ** -16) * (1 + 2 * np.log(V)), (i, g["entropy"][i], H)
+        if top:
+            order = torch.sort(row.float(), descending=True, stable=True).indices[:top].numpy()
+            assert np.array_equal(g["top_id"][i], order), (i, g["top_id"][i], order)
+            a, b = g["top_logprob"][i], lp[order]
+            fin = ~np.isinf(b)
+            assert np.array_equal(np.isinf(a), ~fin) and (np.abs(a[fin] - b[fin]) <= tol[order][fin]).all(), i
+    return got
+
+
+def rows_of(kind, n, V, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, V, generator=g) * 3
+    if kind == "ties":
+        x = torch.randint(-3, 4, (n, V), generator=g).float()
+    elif kind == "flat":
+        x = torch.full((n, V), -1.25)
+    elif kind == "rising":
+        x = torch.sort(x, dim=1).values
+    elif kind == "falling":
+        x = torch.sort(x, dim=1, descending=True).values
+    elif kind == "peaked":
+        x[torch.arange(n), torch.randint(0, V, (n,), generator=g)] = 40.0
+    elif kind == "masked":  # -inf almost everywhere, the type's lowest value in places
+        x = torch.where(torch.rand(n, V, generator=g) < 0.97, -torch.inf, x)
+        x[:, 3] = torch.finfo(torch.float32 if dtype == "f32" else torch.bfloat16).min
+        x[:, V // 2] = 1.0
+    elif kind == "one":     # a single legal token
+        x = torch.full((n, V), -torch.inf)
+        x[torch.arange(n), torch.randint(0, V, (n,), generator=g)] = -7.0
+    elif kind == "large":
+        x = x * 1e4
+    elif kind == "zeros":   # both zeros are one value: the lower index first
+        x = torch.where(torch.rand(n, V, generator=g) < 0.5, 0.0, -0.0)
+    return (x if dtype == "f32" else x.bfloat16()).to(DEV)
+
+
+@pytest.mark.parametrize("kind", ["normal", "ties", "flat", "rising", "falling", "peaked", "masked", "one", "large", "zeros"])
+@pytest.mark.parametrize("dtype,V,top", [("f32", 4096, 20), ("bf16", 4096, 32), ("bf16", 50008, 5), ("f32", 8, 8), ("bf16", 8, 1), ("bf16", 1040, 32),
+                                         ("f32", 24, 20), ("bf16", 151936, 20)])
+def test_rows(kind, dtype, V, top):
+    n = 5 if V < 100000 else 3
+    logits = rows_of(kind, n, V, dtype, V)
+    g = torch.Generator().manual_seed(1)
+    tokens = torch.randint(0, V, (n,), generator=g).to(torch.int32).to(DEV)
+    tokens[0] = logits[0].float().argmax().int()
+    check(make(V, dtype), logits, tokens, top=top)
+
+
+@pytest.mark.parametrize("n", [1, 2, 37, 300, 1500])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_batch_sizes_rows_and_skipped_entries(n, dtype):
+    V = 2056
+    logits = rows_of("normal", n + 9, V, dtype, n).view(1, n + 9, V)
+    g = torch.Generator().manual_seed(n)
+    rows = torch.randint(0, n + 9, (n,), generator=g).to(torch.int32).to(DEV)  # a row may be asked for twice
+    tokens = torch.randint(-V, V, (n,), generator=g).clamp(min=-1).to(torch.int32).to(DEV)
+    check(make(V, dtype), logits, tokens, rows=rows, top=3)
+
+
+@pytest.mark.parametrize("invt", [0.25, 1.7, 40.0])
+def test_temperature(invt):
+    logits = rows_of("normal", 4, 4096, "bf16", 3)
+    check(make(4096, "bf16", invt), logits, torch.tensor([0, 5, 4095, 9], dtype=torch.int32, device=DEV), top=7, invt=invt)
+
+
+@pytest.mark.parametrize("V", [64, 4096, 50008])
+def test_faults_are_reported_and_stay_in_their_rows(V):
+    logits = rows_of("normal", 7, V, "f32", 5)
+    logits[1, V // 3], logits[2, V - 1] = float("nan"), float("inf")
+    logits[3] = -torch.inf
+    isd = make(V, "f32")
+    tokens = torch.tensor([1, 1, 1, 1, 2, 1, 3], dtype=torch.int32, device=DEV)
+    check(isd, logits, tokens, top=4, bad_rows={1, 2, 3})
+    assert isd.isd_read_status() == ST_NONFINITE_LOGIT
+    check(isd, logits[4:], torch.tensor([V, 2, 1 << 30], dtype=torch.int32, device=DEV), top=4)
+    assert isd.isd_read_status() == ST_BAD_TOKEN_ID
+    check(isd, logits[4:], torch.tensor([1, 2, 3], dtype=torch.int32, device=DEV), rows=torch.tensor([0, 3, -1], dtype=torch.int32, device=DEV), top=4)
+    assert isd.isd_read_status() == ST_BAD_TOKEN_ID
+    check(isd, logits[4:], torch.tensor([1, -2, 3], dtype=torch.int32, device=DEV), rows=torch.tensor([0, 99, 2], dtype=torch.int32, device=DEV), top=4)
+    assert isd.isd_read_status() == 0  # a skipped entry's row is not looked at
+
+
+def test_outputs_of_the_caller_and_without_entropy():
+    V = 4096
+    logits = rows_of("normal", 4, V, "bf16", 6)
+    tokens = torch.tensor([4, -1, 7, 9], dtype=torch.int32, device=DEV)
+    isd = make(V, "bf16")
+    full = check(isd, logits, tokens, top=5)
+    out = isd_pkg.alloc_logprobs_out(4, 5, DEV)
+    out["entropy"] = None
+    isd.isd_logprobs(logits, tokens, top_n=5, out=out)
+    assert torch.equal(torch.nan_to_num(out["logprob"]), torch.nan_to_num(full["logprob"])) and torch.equal(out["top_id"], full["top_id"])
+    assert isd.isd_logprobs(logits, tokens[:0])["logprob"].numel() == 0
+    no_top = isd.isd_logprobs(logits, tokens)
+    assert no_top["top_id"].shape == (4, 0) and torch.equal(torch.nan_to_num(no_top["logprob"]), torch.nan_to_num(full["logprob"]))
+
+
+def test_repeats_and_replays_give_the_same_bits():
+    """Rows cut into pieces meet in an order of their own; the result does not depend on it."""
+    V = 151936
+    logits = rows_of("normal", 3, V, "bf16", 8)
+    tokens = torch.tensor([4, 70000, 151935], dtype=torch.int32, device=DEV)
+    isd = make(V, "bf16")
+    first = {k: v.clone() for k, v in isd.isd_logprobs(logits, tokens, top_n=20).items()}
+    out = isd_pkg.alloc_logprobs_out(3, 20, DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        isd.isd_logprobs(logits, tokens, top_n=20, out=out)
+    for _ in range(20):
+        graph.replay()
+        assert all(torch.equal(out[k], first[k]) for k in out)
+
+
+def test_refusals():
+    V = 64
+    isd, logits, tokens = make(V, "f32"), torch.zeros(3, V, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    for a, kw in (((logits.bfloat16(), tokens), {}), ((logits[:, :32], tokens), {}), ((logits, tokens.long()), {}), ((logits, tokens), {"top_n": 33}),
+                  ((logits, tokens), {"top_n": -1}), ((logits[:2], tokens), {}), ((logits, tokens.cpu()), {}),
+                  ((logits, tokens), {"rows": torch.zeros(2, dtype=torch.int32, device=DEV)})):
+        with pytest.raises((isd_pkg.IsdError, RuntimeError)):
+            isd.isd_logprobs(*a, **kw)
+    with pytest.raises(isd_pkg.IsdError):
+        make(8, "f32").isd_logprobs(torch.zeros(3, 8, device=DEV), tokens, top_n=9)
