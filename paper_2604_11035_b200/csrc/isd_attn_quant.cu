@@ -1,106 +1,720 @@
-// isd_attn_quant: strict-causal attention of every slot's query block against its paged 4-bit cache (Sec. 3.1 mask).
-// One CTA per (slot, kv head), a page at a time, fp32 on the CUDA cores: online softmax with two threads per row.
+// isd_attn_quant (sm_100a): strict-causal attention of every slot's ISD query block against its paged 4-bit KV cache
+// (Sec. 3.1 mask; Sec. 3.3 (1) "single paged-only kernel").  Tile layout and codec: include/isd.h.
+//
+// With K = sk (ck - zk) and V = sv (cv - zv) per (token, head), the integers ck - zk and cv - zv (-15..15) are exact in
+// bf16 and every scale is a factor of a whole key:
+//     score[j, row] = sk[j] * ((ck - zk)[j, :] . q[row, :])         out[:, row] = sum_j (cv - zv)[j, :] * (sv[j] p[j, row]) / sum_j p[j, row]
+// so the tensor cores multiply integers, scales meet fp32 scores and probabilities, and the one rounding inside is that
+// of sv * p to bf16 (the operand's type).
+//
+// Layout.  Four-bit codes are a quarter of the bytes of bf16, and what then bounds the kernel is arithmetic: with the
+// query rows as the 128 rows of M, as in the bf16 kernel, a tile of 128 keys would cost two full 128 x 128 x 128
+// products for a block of at most 60 rows.  Here the KEYS are M and the rows are N (a multiple of 16):
+//     S^T[key, row] = K[key, :] Q^T           A = K  from tensor memory (lane = key),   B = Q from shared memory
+//     O^T[dim, row] += V^T[dim, key] P^T      A = V^T from tensor memory (lane = dim),  B = P from shared memory
+// so the tensor cores do the work the rows need, and the decoded tiles never touch shared memory: a thread of the decoding
+// warps owns a key (K) or a dim (V, which the cache stores dim-major within a page), turns its 64 bytes of codes into bf16
+// pairs (one LOP3 each: 128 + c; one subtraction: c - z) and stores them to its lane of tensor memory.
+//
+// Softmax.  A thread owns a key's lane and walks the rows: the running maximum would need a reduction over lanes per
+// tile.  It is replaced by a reference maximum per row that is only raised when some score passes it by more than 2^8
+// (probabilities are then at most 2^8, far from any limit of fp32 or bf16, whose precision does not depend on magnitude): a
+// tile costs one vote of the warpgroup.  Row sums stay in registers per lane and are reduced over lanes once a segment.
+//
+// Warps: 0-3 decode K, 4-7 decode V, 8-11 and 12-15 softmax and epilogue of one half of the rows each, 16 and 18 copy pages
+// (one bulk copy of 2176 bytes holds K and V of a (page, head)), 17 issues the MMAs, 19 stages Q.  Work split and combine
+// pass: isd_attn_split.cuh.  Every wait is bounded, as in the bf16 kernel.
+#include <new>
+
+#include "isd_attn_split.cuh"
 #include "isd_quant.cuh"
 
 namespace {
 
-struct QuantAttnParams {
-  int B, Q, N, Hq, Hkv, G, max_pages;
+constexpr int kQuantThreads = 640;
+constexpr int kStageQ = 8 * kQTile;    // one tile of 128 keys: eight pages' tiles
+constexpr int kQuantSegCost = 4;       // fixed cost of a segment in units of one tile's time
+constexpr int kScaleBufs = 4;          // the K decoders run at most three tiles ahead of the softmax
+
+struct QuantParams : SplitParams {
+  int max_pages, num_pages;
   float scale2;  // sm_scale * log2(e)
-  const int32_t* ctx_len;
-  const int32_t* n_ver;
-  const uint8_t* active;
   const int32_t* page_table;
-  const uint32_t* slot_status;
+  uint32_t* global_status;
   const __nv_bfloat16* q;
-  __nv_bfloat16* out;
-  float* lse;
   const uint8_t* pool;
+  unsigned long long wait_ns;
 };
 
-__global__ void __launch_bounds__(256) attn_quant_kernel(const QuantAttnParams P) {
-  __shared__ float sk[ISD_PAGE][ISD_HEAD_DIM], sv[ISD_PAGE][ISD_HEAD_DIM], ss[128][ISD_PAGE + 1];
-  const int b = blockIdx.x, g = blockIdx.y;
-  pdl_wait();
-  pdl_launch_dependents();
-  if (!P.active[b] || (P.slot_status[b] & (ISD_ST_BAD_PAGE_ID | ISD_ST_SLOT_CAPACITY))) return;
-  const int nv = P.n_ver[b];
-  if (nv < 0 || nv > P.N - 1) return;
-  const int ql = nv + P.N, ctx = P.ctx_len[b];
-  const int row = threadIdx.x >> 1, half = threadIdx.x & 1;
-  const int r = row / P.G, h = g * P.G + row % P.G;
-  const bool ok = r < ql;
-  const size_t at = ((size_t)b * P.Q + (ok ? r : 0)) * P.Hq + h;
-  float m = -INFINITY, l = 0.f, o[64];
+// Sizes that depend on the most rows a block of this context can have (64 or 128).
+template <int RMAX>
+struct Cfg {
+  static constexpr int kStages = RMAX == 64 ? 8 : 4;
+  static constexpr int kA = RMAX == 64 ? 2 : 1;       // buffers of the decoded K and V tiles (64 columns each)
+  static constexpr int kSmQ = 0;                      // [2 segments][2 halves of d][RMAX rows][128 B], 128-byte swizzle
+  static constexpr int kSmP = kSmQ + 2 * RMAX * 256;  // [2 tiles][RMAX / 64 halves of rows][128 keys][128 B], 128-byte swizzle
+  static constexpr int kSmRing = kSmP + 2 * (RMAX / 64) * 16384;
+  static constexpr int kSmBar = kSmRing + kStages * kStageQ;
+  static constexpr int kSmScale = kSmBar + 512;       // [kScaleBufs][128] x {sk * scale2, sv}
+  static constexpr int kSmNegM = kSmScale + kScaleBufs * 128 * 8;  // [128] -reference maximum per row (+inf: none yet)
+  static constexpr int kSmF = kSmNegM + 512;          // [128] factor of a raise
+  static constexpr int kSmRed = kSmF + 512;           // [4 warps][128] warp results
+  static constexpr int kSmPrefix = kSmRed + 2048;
+  static constexpr int kSmSlot = kSmPrefix + (kMaxSmemPrefixSlots + 1) * 4 + 12;
+  static constexpr int kSmemBytes = kSmSlot + kMaxSmemPrefixSlots * 4;
+  static constexpr uint32_t kTmK = 0, kTmV = kTmK + kA * 64, kTmS = kTmV + kA * 64, kTmO = kTmS + 2 * RMAX;
+  static constexpr int kChunks = RMAX / 32;           // chunks of 16 rows of a softmax warpgroup
+  static constexpr int kRegsSoftmax = RMAX == 64 ? 136 : 144, kRegsDecode = 72, kRegsRest = RMAX == 64 ? 64 : 48;
+  static_assert(kTmO + RMAX <= 512 && kSmemBytes <= 232448, "tensor memory / shared memory");
+  // 640 threads are launched with 96 registers each
+  static_assert(2 * 128 * kRegsSoftmax + 2 * 128 * kRegsDecode + 128 * kRegsRest <= 640 * 96, "register split");
+  enum {
+    FULL = 0, EMPTY = FULL + kStages, KFULL = EMPTY + kStages, KFREE = KFULL + kA, VFULL = KFREE + kA, VFREE = VFULL + kA,
+    SCALE = VFREE + kA, SFULL = SCALE + kScaleBufs, PFULL = SFULL + 2, ODONE = PFULL + 2, QFULL = ODONE + 2, QFREE = QFULL + 2,
+    OFREE = QFREE + 2, COUNT
+  };
+  static_assert(COUNT * 8 + 32 <= 512, "barrier block");
+};
+
+#define TMEM_LD16(taddr, v, o)                                                                          \
+  asm volatile(                                                                                         \
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "                                                         \
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"                                 \
+      : "=r"(v[o + 0]), "=r"(v[o + 1]), "=r"(v[o + 2]), "=r"(v[o + 3]), "=r"(v[o + 4]), "=r"(v[o + 5]), \
+        "=r"(v[o + 6]), "=r"(v[o + 7]), "=r"(v[o + 8]), "=r"(v[o + 9]), "=r"(v[o + 10]),                \
+        "=r"(v[o + 11]), "=r"(v[o + 12]), "=r"(v[o + 13]), "=r"(v[o + 14]), "=r"(v[o + 15])             \
+      : "r"(taddr))
+
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+__device__ __forceinline__ void wg_sync(int wg) { asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
+__device__ __forceinline__ bool wg_any(int wg, bool v) {
+  uint32_t r;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbar.red.or.pred q, %2, 128, p;\nselp.u32 %0, 1, 0, q;\n}"
+               : "=r"(r) : "r"((uint32_t)v), "r"(1 + wg) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
-  for (int d = 0; d < 64; ++d) o[d] = 0.f;
-  for (int pg = 0; pg * ISD_PAGE < ctx + ql; ++pg) {
-    const uint8_t* tile = P.pool + ((size_t)P.page_table[(size_t)b * P.max_pages + pg] * P.Hkv + g) * kQTile;
-    const __nv_bfloat16* meta = reinterpret_cast<const __nv_bfloat16*>(tile + kQOffMeta);
-    __syncthreads();
-    for (int i = threadIdx.x; i < ISD_PAGE * ISD_HEAD_DIM; i += 256) {
-      const int t = i / ISD_HEAD_DIM, d = i % ISD_HEAD_DIM;
-      const uint32_t kw = reinterpret_cast<const uint32_t*>(tile)[(d >> 5) * 64 + t * 4 + ((d >> 3) & 3)];
-      const uint32_t vw = reinterpret_cast<const uint32_t*>(tile + kQOffV)[d * 2 + (t >> 3)];
-      const int kc = (kw >> (4 * ((d & 7) >> 1) + 16 * (d & 1))) & 15, vc = (vw >> (4 * ((t & 7) >> 1) + 16 * (t & 1))) & 15;
-      const bool in = pg * ISD_PAGE + t < ctx + ql;
-      sk[t][d] = __bfloat162float(meta[t]) * ((float)kc - (__bfloat162float(meta[16 + t]) - 128.f));
-      sv[t][d] = in ? __bfloat162float(meta[32 + t]) * ((float)vc - (__bfloat162float(meta[48 + t]) - 128.f)) : 0.f;
-    }
-    __syncthreads();
-    float s[8];
+  for (int off = 16; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+  return x;
+}
+
+struct Shared {  // what every role needs
+  uint8_t* smem;
+  uint32_t base, bar0, tmem;
+  volatile int* abort_flag;
+  __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8u * (uint32_t)i; }
+  __device__ __forceinline__ bool wait(int i, uint32_t parity) const { return mbar_wait(bar(i), parity & 1u, abort_flag); }
+};
+
+// ------------------------------------------------------------------------------------------------
+// Softmax and epilogue of one segment by warpgroup wg (0, 1): rows [16 c0, 16 c1) of the block
+// ------------------------------------------------------------------------------------------------
+template <int RMAX>
+__device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Segment& sg, const Shared& S, int wg, uint32_t& n) {
+  using C = Cfg<RMAX>;
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, tl = warp * 32 + lane;  // tl: TMEM lane = key of the tile = dim of O
+  const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
+  const int rows = sg.q_len * P.G, chunks = (rows + 15) >> 4;
+  const int c0 = wg == 0 ? 0 : (chunks + 1) >> 1, c1 = wg == 0 ? (chunks + 1) >> 1 : chunks, mine = c1 - c0;
+  const int cnt = sg.j1 - sg.j0;
+  // the warpgroup's own half of each array (the two may be in different segments)
+  float* neg_m = reinterpret_cast<float*>(S.smem + C::kSmNegM) + wg * 64;
+  float* fac = reinterpret_cast<float*>(S.smem + C::kSmF) + wg * 64;
+  float* red = reinterpret_cast<float*>(S.smem + C::kSmRed) + wg * 64;  // [warp][128]
+  const uint32_t neg_m_a = S.base + C::kSmNegM + wg * 256, fac_a = S.base + C::kSmF + wg * 256;
+  uint64_t l2[C::kChunks * 8];  // row sums of this lane's keys, pairs of rows
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = 0.f;
-    for (int d = 0; d < ISD_HEAD_DIM; ++d) {
-      const float x = __bfloat162float(P.q[at * ISD_HEAD_DIM + d]);
+  for (int i = 0; i < C::kChunks * 8; ++i) l2[i] = 0;
+  if (tl < mine * 16) neg_m[tl] = INFINITY;
+  wg_sync(wg);
+  bool ok = true;
+  for (int i = 0; i < cnt; ++i) {
+    const uint32_t nn = n + (uint32_t)i;
+    const int key = (sg.j0 + i) * kTile + tl;
+    // rows v < vmin do not see this lane's key (row v of the packed block is block row v / G)
+    const bool edge = (sg.j0 + i + 1) * kTile > sg.ctx;
+    const int vmin = key >= sg.kv_len ? 0x7FFFFFFF : (key > sg.ctx ? (key - sg.ctx) * P.G : 0);
+    ok = S.wait(C::SFULL + (int)(nn & 1u), nn >> 1) && S.wait(C::SCALE + (int)(nn % kScaleBufs), nn / kScaleBufs);
+    if (!ok) break;
+    tc_fence_after();
+    const uint2 scl = lds64(S.base + C::kSmScale + ((nn % kScaleBufs) * 128 + (uint32_t)tl) * 8);
+    const float sk = __uint_as_float(scl.x), sv = __uint_as_float(scl.y);
+    const uint64_t sk2 = pack2(sk, sk), sv2 = pack2(sv, sv);
+    const uint32_t ts = S.tmem + C::kTmS + (nn & 1u) * RMAX + (uint32_t)c0 * 16 + lane_base;
+    // x = score (log2 domain) - reference of chunk c's 16 rows; -inf where the row does not see the key.  Returns their maximum.
+    auto arguments = [&](int c, const uint32_t* raw, uint64_t* x) -> float {
+      float mx = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = fmaf(x, sk[half * 8 + j][d], s[j]);
-    }
-    float mx = m;
+      for (int k = 0; k < 4; ++k) {
+        const uint4 nm = lds128(neg_m_a + c * 64 + k * 16);
+        uint64_t a = fma2(pack2(__uint_as_float(raw[4 * k]), __uint_as_float(raw[4 * k + 1])), sk2,
+                          pack2(__uint_as_float(nm.x), __uint_as_float(nm.y)));
+        uint64_t b = fma2(pack2(__uint_as_float(raw[4 * k + 2]), __uint_as_float(raw[4 * k + 3])), sk2,
+                          pack2(__uint_as_float(nm.z), __uint_as_float(nm.w)));
+        float e0, e1, e2, e3;
+        unpack2(a, e0, e1);
+        unpack2(b, e2, e3);
+        if (edge) {
+          const int v = (c0 + c) * 16 + 4 * k;
+          if (v + 0 < vmin) e0 = -INFINITY;
+          if (v + 1 < vmin) e1 = -INFINITY;
+          if (v + 2 < vmin) e2 = -INFINITY;
+          if (v + 3 < vmin) e3 = -INFINITY;
+          a = pack2(e0, e1);
+          b = pack2(e2, e3);
+        }
+        mx = max3(mx, e0, e1);
+        mx = max3(mx, e2, e3);
+        x[2 * k] = a;
+        x[2 * k + 1] = b;
+      }
+      return mx;
+    };
+    // With at most 64 rows the arguments of the whole tile stay in registers between the vote and the exponentials; with
+    // 128 they would not fit beside the row sums, and the scores are read from tensor memory a second time.
+    constexpr bool kKeep = C::kChunks <= 2;
+    uint64_t x2[kKeep ? C::kChunks * 8 : 8];
+    auto all_arguments = [&]() -> float {
+      float mx = -INFINITY;
+      uint32_t raw[kKeep ? C::kChunks * 16 : 16];
+      if (kKeep) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      s[j] = pg * ISD_PAGE + half * 8 + j <= ctx + r ? s[j] * P.scale2 : -INFINITY;
-      mx = fmaxf(mx, s[j]);
-    }
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    const float ref = mx == -INFINITY ? 0.f : mx, keep = exp2f(m - ref);
-    m = mx;
-    l *= keep;
+        for (int c = 0; c < C::kChunks; ++c)
+          if (c < mine) TMEM_LD16(ts + c * 16, raw, (kKeep ? c * 16 : 0));
+        tmem_wait_ld();
+      }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float p = exp2f(s[j] - ref);
-      l += p;
-      ss[row][half * 8 + j] = p;
+      for (int c = 0; c < C::kChunks; ++c)
+        if (c < mine) {
+          if (!kKeep) {
+            TMEM_LD16(ts + c * 16, raw, 0);
+            tmem_wait_ld();
+          }
+          mx = fmaxf(mx, arguments(c, raw + (kKeep ? c * 16 : 0), x2 + (kKeep ? c * 8 : 0)));
+        }
+      return mx;
+    };
+    if (mine > 0) {
+      const bool grow = all_arguments() > 8.f;
+      if (wg_any(wg, grow)) {
+        // ---- raise the reference of this warpgroup's rows to the maximum so far (first tile, and when a score has grown
+        // by more than 2^8): sums and O are scaled by 2^(old - new)
+#pragma unroll 1
+        for (int c = 0; c < mine; ++c) {
+          uint32_t raw[16];
+          TMEM_LD16(ts + c * 16, raw, 0);
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float s = __uint_as_float(raw[k]) * sk;
+            if (edge && (c0 + c) * 16 + k < vmin) s = -INFINITY;
+            s = warp_max(s);
+            if (lane == 0) red[warp * 128 + c * 16 + k] = s;
+          }
+        }
+        wg_sync(wg);
+        if (tl < mine * 16) {
+          const float old = -neg_m[tl];
+          const float m = fmaxf(fmaxf(fmaxf(red[tl], red[128 + tl]), fmaxf(red[256 + tl], red[384 + tl])), old);
+          fac[tl] = (old == -INFINITY || m == old) ? 1.f : ex2f(old - m);  // (no reference yet: sums and O are zero)
+          neg_m[tl] = -m;
+        }
+        wg_sync(wg);
+#pragma unroll
+        for (int c = 0; c < C::kChunks; ++c)
+          if (c < mine) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint4 f = lds128(fac_a + c * 64 + k * 16);
+              l2[c * 8 + 2 * k] = mul2(l2[c * 8 + 2 * k], pack2(__uint_as_float(f.x), __uint_as_float(f.y)));
+              l2[c * 8 + 2 * k + 1] = mul2(l2[c * 8 + 2 * k + 1], pack2(__uint_as_float(f.z), __uint_as_float(f.w)));
+            }
+          }
+        if (i > 0) {
+          // PV(nn - 1) must have finished before O is touched (two barriers: see the bf16 kernel)
+          ok = S.wait(C::ODONE + (int)((nn - 1u) & 1u), (nn - 1u) >> 1);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < mine; ++c) {
+            uint32_t ov[16];
+            const uint32_t to = S.tmem + C::kTmO + (uint32_t)(c0 + c) * 16 + lane_base;
+            TMEM_LD16(to, ov, 0);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) ov[k] = __float_as_uint(__uint_as_float(ov[k]) * fac[c * 16 + k]);
+            TMEM_ST16(to, ov, 0);
+          }
+          tmem_wait_st();
+        }
+        if (kKeep) all_arguments();
+      }
+      // ---- probabilities, row sums, and the operand sv * p (rows of a key are contiguous: MN-major, 128-byte swizzle)
+      const uint32_t pb = S.base + C::kSmP + (nn & 1u) * (RMAX / 64) * 16384 + (uint32_t)tl * 128;
+#pragma unroll
+      for (int c = 0; c < C::kChunks; ++c) {
+        if (c < mine) {
+          uint64_t* x = x2 + (kKeep ? c * 8 : 0);
+          if (!kKeep) {
+            uint32_t raw[16];
+            TMEM_LD16(ts + c * 16, raw, 0);
+            tmem_wait_ld();
+            arguments(c, raw, x);
+          }
+          uint32_t pk[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            float a, b;
+            unpack2(x[k], a, b);
+            const uint64_t p = pack2(ex2f(a), ex2f(b));
+            l2[c * 8 + k] = add2(l2[c * 8 + k], p);
+            float pa, pc;
+            unpack2(mul2(p, sv2), pa, pc);
+            if (edge) {  // a key the row does not see has no part, whatever its scale is
+              const int v = (c0 + c) * 16 + 2 * k;
+              if (v < vmin) pa = 0.f;
+              if (v + 1 < vmin) pc = 0.f;
+            }
+            pk[k] = pack_bf16_cvt(pa, pc);
+          }
+          const int cc = c0 + c;
+          const uint32_t row = pb + (uint32_t)(cc >> 2) * 16384;
+          const uint32_t u = (uint32_t)(cc & 3) * 2, sw = (uint32_t)tl & 7u;
+          sts128(row + ((u ^ sw) << 4), pk[0], pk[1], pk[2], pk[3]);
+          sts128(row + (((u + 1) ^ sw) << 4), pk[4], pk[5], pk[6], pk[7]);
+        }
+      }
+      fence_async_smem();
+      tc_fence_before();
     }
     __syncwarp();
+    if (lane == 0) mbar_arrive(S.bar(C::PFULL + (int)(nn & 1u)));
+  }
+  if (!ok) return false;
+  // ---- row sums over the lanes: exchange halves until lane k of a warp holds the sum of row k of a 32-row group
 #pragma unroll
-    for (int d = 0; d < 64; ++d) {
-      float a = o[d] * keep;
-#pragma unroll 4
-      for (int j = 0; j < ISD_PAGE; ++j) a = fmaf(ss[row][j], sv[j][half * 64 + d], a);
-      o[d] = a;
+  for (int h = 0; h < (C::kChunks + 1) / 2; ++h) {
+    float v[32];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) unpack2(l2[h * 16 + k], v[2 * k], v[2 * k + 1]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+      const bool up = (lane & off) != 0;
+#pragma unroll
+      for (int k = 0; k < off; ++k) {
+        const float give = up ? v[k] : v[k + off], keep = up ? v[k + off] : v[k];
+        v[k] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+      }
+    }
+    if (h * 32 + lane < mine * 16) red[warp * 128 + h * 32 + lane] = v[0];
+  }
+  wg_sync(wg);
+  if (tl < mine * 16) {
+    const float l = (red[tl] + red[128 + tl]) + (red[256 + tl] + red[384 + tl]);
+    const float m = -neg_m[tl];
+    const int v = c0 * 16 + tl;
+    fac[tl] = l == 0.f ? 0.f : 1.f / l;
+    if (v < rows) {
+      if (sg.part_slot >= 0) {
+        // a row of NaN scores never got a reference: let the combine pass see it
+        P.part_ml[((size_t)sg.part_slot * 128 + v) * 2] = l == l ? m : INFINITY;
+        P.part_ml[((size_t)sg.part_slot * 128 + v) * 2 + 1] = l;
+      } else if (P.lse) {
+        P.lse[((size_t)sg.b * P.Q + v / P.G) * P.Hq + sg.g * P.G + v % P.G] = (m + log2f(l)) * kLn2;
+      }
     }
   }
-  l += __shfl_xor_sync(0xffffffffu, l, 1);
-  if (!ok) return;
-  for (int d = 0; d < 64; ++d) P.out[at * ISD_HEAD_DIM + half * 64 + d] = __float2bfloat16_rn(o[d] / l);
-  if (P.lse && half == 0) P.lse[at] = (m + log2f(l)) * 0.6931471805599453f;
+  wg_sync(wg);
+  // ---- O: thread = dim, a column per row
+  const uint32_t last = n + (uint32_t)cnt - 1;
+  ok = S.wait(C::ODONE + (int)(last & 1u), last >> 1);
+  if (!ok) return false;
+  tc_fence_after();
+  const uint32_t to = S.tmem + C::kTmO + (uint32_t)c0 * 16 + lane_base;
+#pragma unroll 1
+  for (int c = 0; c < mine; ++c) {
+    uint32_t ov[16];
+    TMEM_LD16(to + c * 16, ov, 0);
+    tmem_wait_ld();
+    const int v0 = (c0 + c) * 16;
+    if (sg.part_slot >= 0) {
+      float* dst = P.part_o + ((size_t)sg.part_slot * 128 + v0) * 128 + tl;
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (v0 + k < rows) dst[k * 128] = __uint_as_float(ov[k]);
+    } else {
+      int r = v0 / P.G, hg = v0 - r * P.G;
+      __nv_bfloat16* dst = P.out + ((size_t)sg.b * P.Q * P.Hq + sg.g * P.G) * ISD_HEAD_DIM + tl;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        if (v0 + k < rows) dst[((size_t)r * P.Hq + hg) * ISD_HEAD_DIM] = __float2bfloat16_rn(__uint_as_float(ov[k]) * fac[c * 16 + k]);
+        if (++hg == P.G) { hg = 0; ++r; }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(S.bar(C::OFREE));
+  n += (uint32_t)cnt;
+  return true;
+}
+
+template <int RMAX>
+__global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const QuantParams P) {
+  using C = Cfg<RMAX>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Shared S;
+  S.smem = smem;
+  S.base = smem_u32(smem);
+  S.bar0 = S.base + C::kSmBar;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kSmBar + C::COUNT * 8);
+  S.abort_flag = reinterpret_cast<volatile int*>(smem + C::kSmBar + C::COUNT * 8 + 8);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x;
+
+  // ---- set-up that touches nothing an earlier kernel wrote
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kStages; ++i) { mbar_init(S.bar(C::FULL + i), 1); mbar_init(S.bar(C::EMPTY + i), 8); }
+    for (int i = 0; i < C::kA; ++i) {
+      mbar_init(S.bar(C::KFULL + i), 4); mbar_init(S.bar(C::KFREE + i), 1);
+      mbar_init(S.bar(C::VFULL + i), 4); mbar_init(S.bar(C::VFREE + i), 1);
+    }
+    for (int i = 0; i < kScaleBufs; ++i) mbar_init(S.bar(C::SCALE + i), 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(S.bar(C::SFULL + i), 1); mbar_init(S.bar(C::PFULL + i), 8); mbar_init(S.bar(C::ODONE + i), 1);
+      mbar_init(S.bar(C::QFULL + i), 1); mbar_init(S.bar(C::QFREE + i), 1);
+    }
+    mbar_init(S.bar(C::OFREE), 8);
+    *S.abort_flag = (S.base & 1023u) ? 1 : 0;  // the swizzled layouts assume a 1 KiB aligned window
+    *reinterpret_cast<volatile unsigned long long*>(S.abort_flag + 2) = P.wait_ns;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  {  // zero Q, P and the ring: what a ragged tile leaves of them has to be finite
+    uint4* z = reinterpret_cast<uint4*>(smem);
+    for (int i = threadIdx.x; i < C::kSmBar / 16; i += kQuantThreads) z[i] = make_uint4(0, 0, 0, 0);
+  }
+  if (warp == 16) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_async_smem();
+  tc_fence_before();
+  pdl_wait();
+  pdl_launch_dependents();
+  __syncthreads();
+  tc_fence_after();
+  S.tmem = *tmem_slot;
+  const int* prefix = P.tile_prefix;
+  const int* slot_info = nullptr;
+  if (P.B <= kMaxSmemPrefixSlots) {
+    int* sm_prefix = reinterpret_cast<int*>(smem + C::kSmPrefix);
+    int* sm_slot = reinterpret_cast<int*>(smem + C::kSmSlot);
+    block_tile_prefix<kQuantSegCost, kQuantThreads>(P, sm_prefix, sm_slot, reinterpret_cast<int*>(smem + C::kSmRed), cta == 0);
+    prefix = sm_prefix;
+    slot_info = sm_slot;
+  }
+  WorkIter<kQuantSegCost> it;
+  it.init(P, cta, prefix, slot_info);
+  Segment sg;
+  const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+
+  if (warp < 4) {
+    // =========================================================================== K decoders: thread = key of the tile
+    regs_dec<C::kRegsDecode>();
+    uint32_t n = 0;
+    const int key = warp * 32 + lane;
+    const uint32_t in_stage = (uint32_t)(key >> 4) * kQTile, t = (uint32_t)key & 15u;
+    bool ok = true;
+    while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+      for (int j = sg.j0; j < sg.j1; ++j, ++n) {
+        const uint32_t s = n % C::kStages, a = n % C::kA;
+        ok = S.wait(C::FULL + (int)s, n / C::kStages);
+        if (!ok) break;
+        const uint32_t src = S.base + C::kSmRing + s * kStageQ + in_stage;
+        uint4 w[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[c] = lds128(src + c * 256 + t * 16);
+        const uint32_t meta = src + kQOffMeta + t * 2;
+        const float sk = __uint_as_float(lds_u16(meta) << 16) * P.scale2, sv = __uint_as_float(lds_u16(meta + 64) << 16);
+        const uint32_t z = lds_u16(meta + 32) * 0x10001u;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(S.bar(C::EMPTY + (int)s));
+        if (n >= (uint32_t)C::kA) ok = S.wait(C::KFREE + (int)a, n / C::kA - 1);
+        if (!ok) break;
+        tc_fence_after();
+        // QK(n - 2) is done; it was issued after PV(n - 4), which waited until the softmax of tile n - 4 had read its scales
+        asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(S.base + C::kSmScale + ((n % kScaleBufs) * 128 + (uint32_t)key) * 8), "f"(sk), "f"(sv) : "memory");
+        const uint32_t tk = S.tmem + C::kTmK + a * 64 + lane_base;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t o[32];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const uint32_t ww[4] = {w[2 * h + c].x, w[2 * h + c].y, w[2 * h + c].z, w[2 * h + c].w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[c * 16 + u * 4 + e] = sub_zero(codes_to_bf16(ww[u] >> (4 * e)), z);
+          }
+          TMEM_ST32(tk + h * 32, o, 0);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(S.bar(C::KFULL + (int)a));
+          mbar_arrive(S.bar(C::SCALE + (int)(n % kScaleBufs)));
+        }
+      }
+    }
+  } else if (warp < 8) {
+    // =========================================================================== V decoders: thread = dim
+    regs_dec<C::kRegsDecode>();
+    uint32_t n = 0;
+    const int dim = (warp & 3) * 32 + lane;
+    bool ok = true;
+    while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+      for (int j = sg.j0; j < sg.j1; ++j, ++n) {
+        const uint32_t s = n % C::kStages, a = n % C::kA;
+        ok = S.wait(C::FULL + (int)s, n / C::kStages);
+        if (ok && n >= (uint32_t)C::kA) ok = S.wait(C::VFREE + (int)a, n / C::kA - 1);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t src = S.base + C::kSmRing + s * kStageQ;
+        const uint32_t tv = S.tmem + C::kTmV + a * 64 + lane_base;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t o[32];
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const uint32_t pg = src + (uint32_t)(h * 4 + p) * kQTile;
+            const uint2 w = lds64(pg + kQOffV + dim * 8);
+            const uint4 z0 = lds128(pg + kQOffMeta + 96), z1 = lds128(pg + kQOffMeta + 112);
+            const uint32_t z[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              o[p * 8 + e] = sub_zero(codes_to_bf16(w.x >> (4 * e)), z[e]);
+              o[p * 8 + 4 + e] = sub_zero(codes_to_bf16(w.y >> (4 * e)), z[4 + e]);
+            }
+          }
+          TMEM_ST32(tv + h * 32, o, 0);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(S.bar(C::EMPTY + (int)s));
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(S.bar(C::VFULL + (int)a));
+      }
+    }
+  } else if (warp < 16) {
+    // =========================================================================== softmax / epilogue
+    regs_inc<C::kRegsSoftmax>();
+    uint32_t n = 0;
+    bool ok = true;
+    while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+      ok = softmax_segment_q<RMAX>(P, sg, S, (warp - 8) >> 2, n);
+    }
+  } else {
+    regs_dec<C::kRegsRest>();
+    if (warp == 16 || warp == 18) {
+      // ========================================================================= page copies, tiles by turns
+      const uint32_t pw = warp == 16 ? 0u : 1u;
+      uint32_t n = 0;
+      bool ok = true;
+      while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+        const int32_t* pt = P.page_table + (size_t)sg.b * P.max_pages;
+        const int total_pages = (sg.kv_len + ISD_PAGE - 1) / ISD_PAGE;
+        // page ids 32 at a time (4 tiles), one chunk ahead
+        auto load_chunk = [&](int c) -> int {
+          const int pg = sg.j0 * 8 + c * 32 + lane;
+          const int id = pg < total_pages ? pt[pg] : 0;
+          return min(max(id, 0), P.num_pages - 1);
+        };
+        int ids = load_chunk(0), ids_next = load_chunk(1);
+        for (int i = 0; i < sg.j1 - sg.j0; ++i, ++n) {
+          if (i > 0 && (i & 3) == 0) {
+            ids = ids_next;
+            ids_next = load_chunk((i >> 2) + 1);
+          }
+          if ((n & 1u) != pw) continue;
+          const int valid = min(8, total_pages - (sg.j0 + i) * 8);
+          const uint32_t s = n % C::kStages;
+          ok = S.wait(C::EMPTY + (int)s, (n / C::kStages) ^ 1u);
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(S.bar(C::FULL + (int)s), (uint32_t)valid * kQTile);
+          __syncwarp();
+          const int pid = __shfl_sync(0xffffffffu, ids, ((i & 3) << 3) + (lane & 7));
+          if (lane < valid)
+            bulk_g2s(S.base + C::kSmRing + s * kStageQ + lane * kQTile, P.pool + ((size_t)pid * P.Hkv + sg.g) * kQTile, kQTile,
+                     S.bar(C::FULL + (int)s));
+          __syncwarp();
+        }
+      }
+      if (*S.abort_flag) {  // every issued copy must have landed before the CTA may exit
+        for (uint32_t f = (n > (uint32_t)C::kStages ? n - C::kStages : 0); f < n; ++f)
+          if ((f & 1u) == pw)
+            isd_bounded_wait(P.wait_ns, nullptr, [&]() { return mbar_try_wait(S.bar(C::FULL + (int)(f % C::kStages)), (f / C::kStages) & 1u); });
+      }
+    } else if (warp == 17) {
+      // ========================================================================= MMA issuer
+      uint32_t n = 0, seg = 0;
+      bool ok = true;
+      while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+        const int cnt = sg.j1 - sg.j0;
+        const uint32_t ncols = (uint32_t)((sg.q_len * P.G + 15) & ~15);
+        const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((ncols >> 3) << 17) | ((128u >> 4) << 24);
+        const uint32_t idesc_pv = idesc_qk | (1u << 16);  // B (= P) is MN-major
+        ok = S.wait(C::QFULL + (int)(seg & 1u), seg >> 1);
+        if (!ok) break;
+        auto qk = [&](uint32_t nn, bool last) -> bool {
+          const uint32_t a = nn % C::kA;
+          if (!S.wait(C::KFULL + (int)a, nn / C::kA)) return false;
+          // S[nn & 1] is free: PV(nn - 2), issued before, waited for P(nn - 2), which was stored after S(nn - 2) was read
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t qb = S.base + C::kSmQ + (seg & 1u) * RMAX * 256;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              tc_mma_ts(S.tmem + C::kTmS + (nn & 1u) * RMAX, S.tmem + C::kTmK + a * 64 + (uint32_t)k * 8u,
+                        smem_desc(qb + (uint32_t)(k >> 2) * (RMAX * 128) + (uint32_t)(k & 3) * 32u, 16, 1024), idesc_qk, k > 0);
+            tc_commit(S.bar(C::KFREE + (int)a));
+            tc_commit(S.bar(C::SFULL + (int)(nn & 1u)));
+            if (last) tc_commit(S.bar(C::QFREE + (int)(seg & 1u)));
+          }
+          __syncwarp();
+          return true;
+        };
+        auto pv = [&](uint32_t nn, bool first) -> bool {
+          const uint32_t a = nn % C::kA;
+          if (!S.wait(C::VFULL + (int)a, nn / C::kA)) return false;
+          if (!S.wait(C::PFULL + (int)(nn & 1u), nn >> 1)) return false;
+          if (first && seg > 0 && !S.wait(C::OFREE, seg - 1u)) return false;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t pb = S.base + C::kSmP + (nn & 1u) * (RMAX / 64) * 16384;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)  // 16 keys = 8 packed columns of V
+              tc_mma_ts(S.tmem + C::kTmO, S.tmem + C::kTmV + a * 64 + (uint32_t)k * 8u, smem_desc(pb + (uint32_t)k * 2048u, 16384, 1024),
+                        idesc_pv, !(first && k == 0));
+            tc_commit(S.bar(C::VFREE + (int)a));
+            tc_commit(S.bar(C::ODONE + (int)(nn & 1u)));
+          }
+          __syncwarp();
+          return true;
+        };
+        ok = qk(n, cnt == 1);
+        for (int i = 0; i < cnt && ok; ++i) {
+          if (i + 1 < cnt) ok = qk(n + i + 1, i + 2 == cnt);
+          if (ok) ok = pv(n + i, i == 0);
+        }
+        n += (uint32_t)cnt;
+        ++seg;
+      }
+    } else {
+      // ========================================================================= Q: rows of the block, a segment ahead
+      uint32_t seg = 0;
+      bool ok = true;
+      while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+        if (seg >= 2) ok = S.wait(C::QFREE + (int)(seg & 1u), (seg >> 1) - 1u);
+        if (!ok) break;
+        const int rows = sg.q_len * P.G, padded = (rows + 15) & ~15;
+        const uint32_t qb = S.base + C::kSmQ + (seg & 1u) * RMAX * 256;
+        const __nv_bfloat16* src = P.q + ((size_t)sg.b * P.Q * P.Hq + sg.g * P.G) * ISD_HEAD_DIM;
+        const int piece = lane & 15;  // 16 bytes of a row's 256
+        for (int v0 = lane >> 4; v0 < padded; v0 += 8) {  // two rows a step, four steps in flight
+          uint4 x[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int v = v0 + 2 * u;
+            x[u] = make_uint4(0, 0, 0, 0);
+            if (v < rows) x[u] = *reinterpret_cast<const uint4*>(src + ((size_t)(v / P.G) * P.Hq + v % P.G) * ISD_HEAD_DIM + piece * 8);
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const uint32_t v = (uint32_t)(v0 + 2 * u);
+            sts128(qb + (uint32_t)(piece >> 3) * (RMAX * 128) + v * 128 + ((((uint32_t)piece & 7u) ^ (v & 7u)) << 4), x[u].x, x[u].y, x[u].z, x[u].w);
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(S.bar(C::QFULL + (int)(seg & 1u)));
+        ++seg;
+      }
+    }
+  }
+
+  // ---- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *S.abort_flag) atomicOr(P.global_status, ISD_ST_KERNEL_TIMEOUT);
+  if (warp == 16) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(S.tmem) : "memory");
+  }
+}
+
+template <int RMAX>
+cudaError_t launch_main(const isd_ctx* ctx, const QuantParams& P, cudaStream_t stream) {
+  return isd_launch_pdl(attn_quant_kernel<RMAX>, dim3(P.num_ctas), dim3(kQuantThreads), Cfg<RMAX>::kSmemBytes, stream, P);
 }
 
 }  // namespace
 
-int isd_attn_quant_create(isd_ctx*) { return ISD_OK; }
-void isd_attn_quant_destroy(isd_ctx*) {}
+int isd_attn_quant_create(isd_ctx* ctx) {
+  if (cudaMalloc(&ctx->quant_prefix, sizeof(int) * (ctx->cfg.batch + 1)) != cudaSuccess) return ISD_ERR_NO_MEMORY;
+  if (cudaFuncSetAttribute(attn_quant_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn_quant_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmemBytes) != cudaSuccess)
+    return ISD_ERR_CUDA;
+  return ISD_OK;
+}
 
-int isd_launch_attn_quant(isd_ctx* ctx, const isd_batch_state* st, const void* q, const void*, const void*,
+void isd_attn_quant_destroy(isd_ctx* ctx) { cudaFree(ctx->quant_prefix); }
+
+int isd_launch_attn_quant(isd_ctx* ctx, const isd_batch_state* st, const void* q, const void* k_new, const void* v_new,
                           void* kv_pool, void* out, float* lse, cudaStream_t stream) {
+  (void)k_new; (void)v_new;  // already appended to the pages
   const isd_config& c = ctx->cfg;
-  QuantAttnParams P;
-  P.B = c.batch; P.Q = ctx->Q; P.N = c.stride; P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads; P.G = ctx->G; P.max_pages = c.max_pages_per_slot;
-  P.scale2 = ctx->sm_scale * 1.4426950408889634f;
-  P.ctx_len = st->ctx_len; P.n_ver = st->n_ver; P.active = st->active; P.page_table = st->page_table; P.slot_status = st->slot_status;
+  QuantParams P;
+  P.B = c.batch; P.Q = ctx->Q; P.N = c.stride; P.Hq = c.n_q_heads; P.Hkv = c.n_kv_heads; P.G = ctx->G;
+  P.max_pages = c.max_pages_per_slot; P.num_pages = c.num_pages;
+  P.scale2 = ctx->sm_scale * kLog2e;
+  P.ctx_len = st->ctx_len; P.n_ver = st->n_ver; P.active = st->active; P.page_table = st->page_table;
+  P.slot_status = st->slot_status; P.global_status = ctx->global_status;
   P.q = (const __nv_bfloat16*)q; P.out = (__nv_bfloat16*)out; P.lse = lse; P.pool = (const uint8_t*)kv_pool;
-  const cudaError_t e = isd_launch_pdl(attn_quant_kernel, dim3(c.batch, c.n_kv_heads), dim3(256), 0, stream, P);
-  ctx->launches++;
+  P.tile_prefix = ctx->quant_prefix; P.part_o = ctx->attn_part_o; P.part_ml = ctx->attn_part_ml;
+  P.num_ctas = ctx->attn_ctas;
+  P.wait_ns = ctx->wait_ns;
+  cudaError_t e = cudaSuccess;
+  if (c.batch > kMaxSmemPrefixSlots) e = isd_launch_pdl(attn_plan_kernel<kQuantSegCost>, dim3(1), dim3(1024), 0, stream, P);
+  if (ctx->ev_attn0) cudaEventRecord(ctx->ev_attn0, stream);
+  if (e == cudaSuccess) e = ctx->G * ctx->Q <= 64 ? launch_main<64>(ctx, P, stream) : launch_main<128>(ctx, P, stream);
+  if (ctx->ev_attn1) cudaEventRecord(ctx->ev_attn1, stream);
+  if (e == cudaSuccess) e = isd_launch_pdl(attn_combine_kernel<kQuantSegCost, false>, dim3(P.num_ctas), dim3(kCombineThreads), 0, stream, P);
+  ctx->launches += 2 + (c.batch > kMaxSmemPrefixSlots ? 1 : 0);
   return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }

@@ -1,0 +1,299 @@
+// How the tensor-core attention kernels share a batch among their persistent CTAs: all (slot, kv head) key ranges are laid
+// end to end in units of 128-key tiles and cut into equal contiguous shares.  kSegCost is the fixed cost of a segment in
+// units of one tile's time, measured for each kernel.
+#pragma once
+#include "isd_tc.cuh"
+
+namespace {
+
+constexpr int kTile = 128;  // keys per tile
+constexpr int kMaxSmemPrefixSlots = 1024;
+
+struct SplitParams {
+  int B, N, Hkv, num_ctas;
+  const int32_t* ctx_len;
+  const int32_t* n_ver;
+  const uint8_t* active;
+  const uint32_t* slot_status;
+  int* tile_prefix;  // [B + 1] split-axis length (tiles + kSegCost) per kv head, exclusive prefix over slots
+  int Q, Hq, G;
+  __nv_bfloat16* out;
+  float* lse;
+  float* part_o;     // [ctas * 2][128][128]
+  float* part_ml;    // [ctas * 2][128][2]
+};
+
+// ------------------------------------------------------------------------------------------------
+// Work split: identical, independent enumeration in every warp role
+// ------------------------------------------------------------------------------------------------
+struct Segment {
+  int b, g;      // slot, kv head
+  int j0, j1;    // tiles [j0, j1) of the pair
+  int T;         // tiles of the whole pair
+  int kv_len;    // ctx_len + q_len
+  int ctx, q_len;
+  int part_slot; // scratch slot when the segment does not cover the whole pair, else -1
+};
+
+// Units of the split axis per CTA.  Small batches do not fill the machine: below kMinShare units a share would
+// be mostly fixed cost (Q staging, pipeline fill, a partial result of 64 KB that the combine kernel reads back), so
+// fewer CTAs take longer shares and the rest leave at once.
+constexpr int kMinShare = 8;  // 12 and 16 measured slower at batch 1, equal at batch 8
+__device__ __forceinline__ long long share_units(long long total, int num_ctas) {
+  const long long per = (total + num_ctas - 1) / num_ctas;
+  return per < kMinShare ? kMinShare : per;
+}
+
+template <int kSegCost>
+struct WorkIter {
+  const int* prefix;
+  const int* slot_info;  // ctx_len | q_len << 24 per slot in shared memory, or nullptr (read the state arrays)
+  int B, Hkv, b;
+  long long t, t_begin, t_end;
+  __device__ void init(const SplitParams& P, int cta, const int* prefix_, const int* slot_info_) {
+    prefix = prefix_;
+    slot_info = slot_info_;
+    B = P.B; Hkv = P.Hkv;
+    const long long total = (long long)prefix[B] * Hkv;
+    const long long per = share_units(total, P.num_ctas);
+    t_begin = t = (long long)cta * per;
+    t_end = t + per < total ? t + per : total;
+    // first slot whose range ends after t
+    int lo = 0, hi = B;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if ((long long)prefix[mid + 1] * Hkv > t) hi = mid; else lo = mid + 1;
+    }
+    b = lo;
+  }
+  __device__ bool next(const SplitParams& P, int cta, Segment& s) {
+    for (;;) {
+      if (t >= t_end) return false;
+      while (b < B && (long long)prefix[b + 1] * Hkv <= t) ++b;
+      if (b >= B) return false;
+      // positions of a pair on the split axis: kSegCost units of fixed cost, then its tiles
+      const int Tv = prefix[b + 1] - prefix[b];
+      const long long off = t - (long long)prefix[b] * Hkv;
+      const int v0 = (int)(off % Tv);
+      const long long room = t_end - t;
+      const int v1 = (long long)(Tv - v0) <= room ? Tv : v0 + (int)room;
+      const bool first = (t == t_begin);
+      t += v1 - v0;
+      const int T = Tv - kSegCost;
+      s.j0 = v0 > kSegCost ? v0 - kSegCost : 0;
+      s.j1 = v1 > kSegCost ? v1 - kSegCost : 0;
+      if (s.j1 <= s.j0) continue;  // only (part of) the fixed-cost units of the pair fell into this share
+      s.b = b; s.T = T;
+      s.g = (int)(off / Tv);
+      if (slot_info) {
+        const int w = slot_info[b];
+        s.ctx = w & 0xFFFFFF;
+        s.q_len = (int)((unsigned)w >> 24);
+      } else {
+        s.ctx = P.ctx_len[b];
+        s.q_len = P.n_ver[b] + P.N;
+      }
+      s.kv_len = s.ctx + s.q_len;
+      const bool whole = (s.j0 == 0 && s.j1 == T);
+      s.part_slot = whole ? -1 : cta * 2 + (first ? 0 : 1);
+      return true;
+    }
+  }
+};
+
+// Length of a slot's (slot, kv head) pairs on the split axis: its 128-key tiles plus kSegCost units for the
+// fixed cost of a segment (Q staging, pipeline fill and drain, epilogue: measured at about the time of four
+// tiles).  Shares of equal length on this axis take equal time whether they hold a few long pairs or many
+// short ones; with tiles alone the CTAs with the most segments finished 10 % after the average.
+template <int kSegCost>
+__device__ __forceinline__ int slot_tiles(const SplitParams& P, int b) {
+  if (b >= P.B || !P.active[b]) return 0;
+  const int nv = P.n_ver[b];
+  const int ctx = P.ctx_len[b];
+  const bool ok = nv >= 0 && nv <= P.N - 1 && ctx >= 0 &&
+                  (P.slot_status[b] & (ISD_ST_BAD_PAGE_ID | ISD_ST_SLOT_CAPACITY)) == 0;
+  return ok ? (ctx + nv + P.N + kTile - 1) / kTile + kSegCost : 0;
+}
+
+// Exclusive prefix of tiles per slot, computed by the 256 threads of a main-kernel CTA into shared
+// memory (batches up to kMaxSmemPrefixSlots); CTA 0 also publishes it for the combine kernel.
+template <int kSegCost, int kThreads>
+__device__ void block_tile_prefix(const SplitParams& P, int* sm_prefix, int* sm_slot, int* sm_warp, bool publish) {
+  int carry = 0;
+  for (int base = 0; base < P.B; base += kThreads) {
+    const int b = base + threadIdx.x;
+    const int tiles = slot_tiles<kSegCost>(P, b);
+    if (b < P.B && tiles > 0) sm_slot[b] = (P.ctx_len[b] & 0xFFFFFF) | ((P.n_ver[b] + P.N) << 24);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int inc = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    if (lane == 31) sm_warp[warp] = inc;
+    __syncthreads();
+    int woff = 0, tot = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+      const int x = sm_warp[w];
+      if (w < warp) woff += x;
+      tot += x;
+    }
+    if (b < P.B) {
+      const int excl = carry + woff + inc - tiles;
+      sm_prefix[b] = excl;
+      if (publish) P.tile_prefix[b] = excl;
+    }
+    carry += tot;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    sm_prefix[P.B] = carry;
+    if (publish) P.tile_prefix[P.B] = carry;
+  }
+  __syncthreads();
+}
+
+// ------------------------------------------------------------------------------------------------
+// Plan for batches too large for the in-kernel prefix: tiles per slot and their exclusive prefix
+// ------------------------------------------------------------------------------------------------
+template <int kSegCost>
+__global__ void __launch_bounds__(1024) attn_plan_kernel(const SplitParams P) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ int sm_warp[33];
+  __shared__ int sm_carry;
+  if (threadIdx.x == 0) sm_carry = 0;
+  __syncthreads();
+  for (int base = 0; base < P.B; base += 1024) {
+    const int b = base + threadIdx.x;
+    const int tiles = slot_tiles<kSegCost>(P, b);
+    // inclusive scan
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int inc = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    if (lane == 31) sm_warp[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+      int w = sm_warp[lane], winc = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, winc, o);
+        if (lane >= o) winc += v;
+      }
+      sm_warp[lane] = winc - w;
+      if (lane == 31) sm_warp[32] = winc;
+    }
+    __syncthreads();
+    const int excl = sm_carry + sm_warp[warp] + inc - tiles;
+    if (b < P.B) P.tile_prefix[b] = excl;
+    __syncthreads();
+    if (threadIdx.x == 0) sm_carry += sm_warp[32];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) P.tile_prefix[P.B] = sm_carry;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Combine: pairs whose tiles were split over several CTAs (log-sum-exp merge of the partials)
+// ------------------------------------------------------------------------------------------------
+// One CTA per share of the main kernel: CTA c merges the pair that starts inside share c and runs on
+// into later shares (every split pair has exactly one such share).  The kernel is pure latency (a few
+// dependent rounds of small loads), so it is laid out wide: the slot of the share's last tile is found by
+// a counting vote over the tile prefix instead of a binary search of dependent loads, and one warp per
+// block row merges all partials of its row in a single round.
+constexpr int kCombineThreads = 1024;
+template <int kSegCost, bool kReplicated>
+__global__ void __launch_bounds__(kCombineThreads) attn_combine_kernel(const SplitParams P) {
+  const int c0 = blockIdx.x;
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long total = (long long)P.tile_prefix[P.B] * P.Hkv;
+  if (total == 0) return;
+  const long long per = share_units(total, P.num_ctas);
+  const long long t_last = ((long long)(c0 + 1) * per < total ? (long long)(c0 + 1) * per : total) - 1;
+  if (t_last < (long long)c0 * per) return;  // empty share
+  // slot of the share's last tile = number of slots whose tiles all lie at or before t_last
+  __shared__ int sm_cnt;
+  if (threadIdx.x == 0) sm_cnt = 0;
+  __syncthreads();
+  {
+    int cnt = 0;
+    for (int i = threadIdx.x; i < P.B; i += kCombineThreads)
+      cnt += ((long long)P.tile_prefix[i + 1] * P.Hkv <= t_last) ? 1 : 0;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) cnt += __shfl_xor_sync(0xffffffffu, cnt, off);
+    if ((threadIdx.x & 31) == 0 && cnt) atomicAdd(&sm_cnt, cnt);
+  }
+  __syncthreads();
+  const int b = sm_cnt;
+  const int T = P.tile_prefix[b + 1] - P.tile_prefix[b];  // on the split axis: kSegCost units, then the tiles
+  const int g = (int)((t_last - (long long)P.tile_prefix[b] * P.Hkv) / T);
+  const long long p0 = (long long)P.tile_prefix[b] * P.Hkv + (long long)g * T, p1 = p0 + T;
+  const int c_first = (int)((p0 + kSegCost) / per), c_last = (int)((p1 - 1) / per);  // shares that hold tiles of the pair
+  if (c_first != c0 || c_last == c0) return;  // merged by an earlier share, or written directly
+  const int q_len = P.n_ver[b] + P.N;
+  const int rows_valid = q_len * P.G;
+  // kReplicated: replicas of a row (the bf16 kernel's key split across lane groups) are further partials
+  const int F = !kReplicated ? 1 : rows_valid > 64 ? 1 : (rows_valid > 32 ? 2 : 4);
+  const int RG = 128 / F;
+  const int lane = threadIdx.x & 31;
+  const int n_part = (c_last - c_first + 1) * F;  // partials of a row: lane i < n_part fetches the i-th (max, sum)
+  for (int row = threadIdx.x >> 5; row < rows_valid; row += kCombineThreads / 32) {
+    float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int base = 0; base < n_part; base += 32) {
+      // one round of loads for up to 32 partials: every lane reads one (max, sum) pair
+      float m_i = -INFINITY, l_i = 0.f;
+      size_t rr_i = 0;
+      if (base + lane < n_part) {
+        const int c = c_first + (base + lane) / F, pp = (base + lane) % F;
+        const int slot = c * 2 + (((long long)c * per >= p0) ? 0 : 1);
+        rr_i = (size_t)slot * 128 + pp * RG + row;
+        const float2 ml = *reinterpret_cast<const float2*>(P.part_ml + rr_i * 2);
+        m_i = ml.x;
+        l_i = ml.y;
+      }
+      float Mn = m_i;
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) Mn = fmaxf(Mn, __shfl_xor_sync(0xffffffffu, Mn, off));
+      Mn = fmaxf(Mn, M);
+      const float keep = (M == -INFINITY) ? 0.f : ex2f(M - Mn);
+      L *= keep;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] *= keep;
+      M = Mn;
+      const float w_i = (m_i == -INFINITY) ? 0.f : ex2f(m_i - M);
+      const int cnt = min(32, n_part - base);
+      for (int i = 0; i < cnt; i += 4) {  // four independent loads in flight
+        float4 o[4];
+        float w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int ii = min(i + u, cnt - 1);
+          const float wu = __shfl_sync(0xffffffffu, w_i, ii);
+          const float lu = __shfl_sync(0xffffffffu, l_i, ii);
+          const size_t rr = __shfl_sync(0xffffffffu, (unsigned long long)rr_i, ii);
+          w[u] = (i + u < cnt) ? wu : 0.f;
+          L += lu * w[u];
+          o[u] = *reinterpret_cast<const float4*>(P.part_o + rr * 128 + lane * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          acc[0] += o[u].x * w[u]; acc[1] += o[u].y * w[u]; acc[2] += o[u].z * w[u]; acc[3] += o[u].w * w[u];
+        }
+      }
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const int r = row / P.G, hg = row % P.G;
+    const size_t o_off = (((size_t)b * P.Q + r) * P.Hq + g * P.G + hg) * ISD_HEAD_DIM + lane * 4;
+    *reinterpret_cast<uint2*>(P.out + o_off) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+    if (P.lse && lane == 0) P.lse[((size_t)b * P.Q + r) * P.Hq + g * P.G + hg] = (M + log2f(L)) * kLn2;
+  }
+}
+
+}  // namespace

@@ -26,11 +26,11 @@
 #include <cuda.h>
 #include <new>
 
-#include "isd_internal.cuh"
+#include "isd_attn_split.cuh"
+#include "isd_tc.cuh"
 
 namespace {
 
-constexpr int kTile = 128;                 // keys per tile
 constexpr int kStageBytes = 32768;         // one K or V tile: [half(2)][page(8)][tok(16)][128 B]
 constexpr int kStages = 6;
 constexpr int kSegCost = 4;  // fixed cost of a segment in units of one tile's time (split axis), measured
@@ -44,339 +44,22 @@ constexpr int kSmXchg = kSmMl + 1024;   // [3][32 rows] or [1][64 rows] x 32 flo
 // its S buffer once the scores are in registers), O, and the query block Q (bf16 pairs, 64 columns)
 constexpr uint32_t kTmS = 0, kTmO = 256, kTmQ = 384;  // Q: two buffers of 64 columns (segment parity)
 constexpr int kSmPrefix = kSmXchg + 12288;  // tile prefix over slots when the batch fits (else it stays in global memory)
-constexpr int kMaxSmemPrefixSlots = 1024;
 constexpr int kSmSlot = kSmPrefix + (kMaxSmemPrefixSlots + 1) * 4 + 12;  // per slot: ctx_len | q_len << 24 (with the prefix)
 constexpr int kSmemBytes = kSmSlot + kMaxSmemPrefixSlots * 4;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 // barrier slots (8 bytes each) inside the barrier block
 enum { BAR_FULL = 0, BAR_EMPTY = kStages, BAR_SFULL = 2 * kStages,
        BAR_PFULL = 2 * kStages + 2, BAR_ODONE = 2 * kStages + 4, BAR_OFREE = 2 * kStages + 6,
        BAR_QFULL = 2 * kStages + 7, BAR_COUNT = 2 * kStages + 8 };
 
-struct TcParams {
-  int B, Q, N, Hq, Hkv, G, max_pages, num_pages;
+struct TcParams : SplitParams {
+  int max_pages, num_pages;
   float scale2;  // sm_scale * log2(e)
-  const int32_t* ctx_len;
-  const int32_t* n_ver;
-  const uint8_t* active;
   const int32_t* page_table;
-  const uint32_t* slot_status;
   uint32_t* global_status;
   const __nv_bfloat16* q;
-  __nv_bfloat16* out;
-  float* lse;
-  int* tile_prefix;  // [B + 1] split-axis length (tiles + kSegCost) per kv head, exclusive prefix over slots
-  float* part_o;     // [ctas * 2][128][128]
-  float* part_ml;    // [ctas * 2][128][2]
-  int num_ctas;
   unsigned long long wait_ns;  // time limit of a device-side wait
 };
-
-// ------------------------------------------------------------------------------------------------
-// PTX wrappers
-// ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n.reg .pred p;\n"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-      "selp.u32 %0, 1, 0, p;\n}"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-
-// Bounded wait: returns false (and raises the abort flag) when the time limit is reached or another thread of
-// the CTA has given up.  The limit (nanoseconds) sits in shared memory two words behind the abort flag.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const unsigned long long budget = *reinterpret_cast<const volatile unsigned long long*>(abort_flag + 2);
-  return isd_bounded_wait(budget, abort_flag, [&]() { return mbar_try_wait(bar, parity); });
-}
-
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
-}
-
-// One lane of a converged warp; unlike `lane == 0` the compiler keeps the surrounding code uniform, so
-// that MMA descriptors stay in uniform registers instead of being moved there one by one.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t pred = 0;
-  asm volatile(
-      "{\n.reg .b32 rx;\n.reg .pred px;\n"
-      "elect.sync rx|px, 0xffffffff;\n"
-      "selp.u32 %0, 1, 0, px;\n}"
-      : "=r"(pred));
-  return pred != 0;
-}
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-
-// A operand read from tensor memory (row = lane, 2 bf16 per 32-bit column), B from shared memory
-__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accum) {
-  asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accum) : "memory");
-}
-
-
-// K-major / MN-major shared-memory matrix descriptor, 128-byte swizzle, descriptor version 1
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  const uint32_t lo = ((addr & 0x3FFFFu) >> 4) | ((lbo_bytes >> 4) << 16);
-  const uint32_t hi = (sbo_bytes >> 4) | (1u << 14) | (2u << 29);
-  return ((uint64_t)hi << 32) | lo;
-}
-
-#define TMEM_LD32(taddr, v, o)                                                                          \
-  asm volatile(                                                                                         \
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "                                                         \
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25," \
-      "%26,%27,%28,%29,%30,%31}, [%32];"                                                                \
-      : "=r"(v[o + 0]), "=r"(v[o + 1]), "=r"(v[o + 2]), "=r"(v[o + 3]), "=r"(v[o + 4]), "=r"(v[o + 5]), \
-        "=r"(v[o + 6]), "=r"(v[o + 7]), "=r"(v[o + 8]), "=r"(v[o + 9]), "=r"(v[o + 10]),                \
-        "=r"(v[o + 11]), "=r"(v[o + 12]), "=r"(v[o + 13]), "=r"(v[o + 14]), "=r"(v[o + 15]),            \
-        "=r"(v[o + 16]), "=r"(v[o + 17]), "=r"(v[o + 18]), "=r"(v[o + 19]), "=r"(v[o + 20]),            \
-        "=r"(v[o + 21]), "=r"(v[o + 22]), "=r"(v[o + 23]), "=r"(v[o + 24]), "=r"(v[o + 25]),            \
-        "=r"(v[o + 26]), "=r"(v[o + 27]), "=r"(v[o + 28]), "=r"(v[o + 29]), "=r"(v[o + 30]),            \
-        "=r"(v[o + 31])                                                                                 \
-      : "r"(taddr))
-
-#define TMEM_ST32(taddr, v, o)                                                                          \
-  asm volatile(                                                                                         \
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "                                                   \
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26," \
-      "%27,%28,%29,%30,%31,%32};"                                                                       \
-      ::"r"(taddr), "r"(v[o + 0]), "r"(v[o + 1]), "r"(v[o + 2]), "r"(v[o + 3]), "r"(v[o + 4]),          \
-        "r"(v[o + 5]), "r"(v[o + 6]), "r"(v[o + 7]), "r"(v[o + 8]), "r"(v[o + 9]), "r"(v[o + 10]),      \
-        "r"(v[o + 11]), "r"(v[o + 12]), "r"(v[o + 13]), "r"(v[o + 14]), "r"(v[o + 15]), "r"(v[o + 16]), \
-        "r"(v[o + 17]), "r"(v[o + 18]), "r"(v[o + 19]), "r"(v[o + 20]), "r"(v[o + 21]), "r"(v[o + 22]), \
-        "r"(v[o + 23]), "r"(v[o + 24]), "r"(v[o + 25]), "r"(v[o + 26]), "r"(v[o + 27]), "r"(v[o + 28]), \
-        "r"(v[o + 29]), "r"(v[o + 30]), "r"(v[o + 31])                                                  \
-      : "memory")
-
-#define TMEM_ST16(taddr, v, o)                                                                          \
-  asm volatile(                                                                                         \
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "                                                   \
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"                                       \
-      ::"r"(taddr), "r"(v[o + 0]), "r"(v[o + 1]), "r"(v[o + 2]), "r"(v[o + 3]), "r"(v[o + 4]),          \
-        "r"(v[o + 5]), "r"(v[o + 6]), "r"(v[o + 7]), "r"(v[o + 8]), "r"(v[o + 9]), "r"(v[o + 10]),      \
-        "r"(v[o + 11]), "r"(v[o + 12]), "r"(v[o + 13]), "r"(v[o + 14]), "r"(v[o + 15])                  \
-      : "memory")
-
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ float ex2f(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<uint32_t*>(&h);
-}
-
-// bf16 pair (a in the low half, b in the high half) with the conversion instruction: one instruction instead of
-// three, which matters more than the pipe it runs on -- the softmax warps are bound by instruction issue (one warp
-// per scheduler), not by the transcendental unit
-__device__ __forceinline__ uint32_t pack_bf16_cvt(float a, float b) {
-  uint32_t d;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
-  return d;
-}
-
-// ------------------------------------------------------------------------------------------------
-// Work split: identical, independent enumeration in every warp role
-// ------------------------------------------------------------------------------------------------
-struct Segment {
-  int b, g;      // slot, kv head
-  int j0, j1;    // tiles [j0, j1) of the pair
-  int T;         // tiles of the whole pair
-  int kv_len;    // ctx_len + q_len
-  int ctx, q_len;
-  int part_slot; // scratch slot when the segment does not cover the whole pair, else -1
-};
-
-// Units of the split axis per CTA.  Small batches do not fill the machine: below kMinShare units a share would
-// be mostly fixed cost (Q staging, pipeline fill, a partial result of 64 KB that the combine kernel reads back), so
-// fewer CTAs take longer shares and the rest leave at once.
-constexpr int kMinShare = 8;  // 12 and 16 measured slower at batch 1, equal at batch 8
-__device__ __forceinline__ long long share_units(long long total, int num_ctas) {
-  const long long per = (total + num_ctas - 1) / num_ctas;
-  return per < kMinShare ? kMinShare : per;
-}
-
-struct WorkIter {
-  const int* prefix;
-  const int* slot_info;  // ctx_len | q_len << 24 per slot in shared memory, or nullptr (read the state arrays)
-  int B, Hkv, b;
-  long long t, t_begin, t_end;
-  __device__ void init(const TcParams& P, int cta, const int* prefix_, const int* slot_info_) {
-    prefix = prefix_;
-    slot_info = slot_info_;
-    B = P.B; Hkv = P.Hkv;
-    const long long total = (long long)prefix[B] * Hkv;
-    const long long per = share_units(total, P.num_ctas);
-    t_begin = t = (long long)cta * per;
-    t_end = t + per < total ? t + per : total;
-    // first slot whose range ends after t
-    int lo = 0, hi = B;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if ((long long)prefix[mid + 1] * Hkv > t) hi = mid; else lo = mid + 1;
-    }
-    b = lo;
-  }
-  __device__ bool next(const TcParams& P, int cta, Segment& s) {
-    for (;;) {
-      if (t >= t_end) return false;
-      while (b < B && (long long)prefix[b + 1] * Hkv <= t) ++b;
-      if (b >= B) return false;
-      // positions of a pair on the split axis: kSegCost units of fixed cost, then its tiles
-      const int Tv = prefix[b + 1] - prefix[b];
-      const long long off = t - (long long)prefix[b] * Hkv;
-      const int v0 = (int)(off % Tv);
-      const long long room = t_end - t;
-      const int v1 = (long long)(Tv - v0) <= room ? Tv : v0 + (int)room;
-      const bool first = (t == t_begin);
-      t += v1 - v0;
-      const int T = Tv - kSegCost;
-      s.j0 = v0 > kSegCost ? v0 - kSegCost : 0;
-      s.j1 = v1 > kSegCost ? v1 - kSegCost : 0;
-      if (s.j1 <= s.j0) continue;  // only (part of) the fixed-cost units of the pair fell into this share
-      s.b = b; s.T = T;
-      s.g = (int)(off / Tv);
-      if (slot_info) {
-        const int w = slot_info[b];
-        s.ctx = w & 0xFFFFFF;
-        s.q_len = (int)((unsigned)w >> 24);
-      } else {
-        s.ctx = P.ctx_len[b];
-        s.q_len = P.n_ver[b] + P.N;
-      }
-      s.kv_len = s.ctx + s.q_len;
-      const bool whole = (s.j0 == 0 && s.j1 == T);
-      s.part_slot = whole ? -1 : cta * 2 + (first ? 0 : 1);
-      return true;
-    }
-  }
-};
-
-// Length of a slot's (slot, kv head) pairs on the split axis: its 128-key tiles plus kSegCost units for the
-// fixed cost of a segment (Q staging, pipeline fill and drain, epilogue: measured at about the time of four
-// tiles).  Shares of equal length on this axis take equal time whether they hold a few long pairs or many
-// short ones; with tiles alone the CTAs with the most segments finished 10 % after the average.
-__device__ __forceinline__ int slot_tiles(const TcParams& P, int b) {
-  if (b >= P.B || !P.active[b]) return 0;
-  const int nv = P.n_ver[b];
-  const int ctx = P.ctx_len[b];
-  const bool ok = nv >= 0 && nv <= P.N - 1 && ctx >= 0 &&
-                  (P.slot_status[b] & (ISD_ST_BAD_PAGE_ID | ISD_ST_SLOT_CAPACITY)) == 0;
-  return ok ? (ctx + nv + P.N + kTile - 1) / kTile + kSegCost : 0;
-}
-
-// Exclusive prefix of tiles per slot, computed by the 256 threads of a main-kernel CTA into shared
-// memory (batches up to kMaxSmemPrefixSlots); CTA 0 also publishes it for the combine kernel.
-__device__ void block_tile_prefix(const TcParams& P, int* sm_prefix, int* sm_slot, int* sm_warp, bool publish) {
-  int carry = 0;
-  for (int base = 0; base < P.B; base += kThreads) {
-    const int b = base + threadIdx.x;
-    const int tiles = slot_tiles(P, b);
-    if (b < P.B && tiles > 0) sm_slot[b] = (P.ctx_len[b] & 0xFFFFFF) | ((P.n_ver[b] + P.N) << 24);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = tiles;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
-    }
-    if (lane == 31) sm_warp[warp] = inc;
-    __syncthreads();
-    int woff = 0, tot = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-      const int x = sm_warp[w];
-      if (w < warp) woff += x;
-      tot += x;
-    }
-    if (b < P.B) {
-      const int excl = carry + woff + inc - tiles;
-      sm_prefix[b] = excl;
-      if (publish) P.tile_prefix[b] = excl;
-    }
-    carry += tot;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
-    sm_prefix[P.B] = carry;
-    if (publish) P.tile_prefix[P.B] = carry;
-  }
-  __syncthreads();
-}
-
-// ------------------------------------------------------------------------------------------------
-// Plan for batches too large for the in-kernel prefix: tiles per slot and their exclusive prefix
-// ------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(1024) attn_plan_kernel(const TcParams P) {
-  pdl_wait();
-  pdl_launch_dependents();
-  __shared__ int sm_warp[33];
-  __shared__ int sm_carry;
-  if (threadIdx.x == 0) sm_carry = 0;
-  __syncthreads();
-  for (int base = 0; base < P.B; base += 1024) {
-    const int b = base + threadIdx.x;
-    const int tiles = slot_tiles(P, b);
-    // inclusive scan
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = tiles;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
-    }
-    if (lane == 31) sm_warp[warp] = inc;
-    __syncthreads();
-    if (warp == 0) {
-      int w = sm_warp[lane], winc = w;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, winc, o);
-        if (lane >= o) winc += v;
-      }
-      sm_warp[lane] = winc - w;
-      if (lane == 31) sm_warp[32] = winc;
-    }
-    __syncthreads();
-    const int excl = sm_carry + sm_warp[warp] + inc - tiles;
-    if (b < P.B) P.tile_prefix[b] = excl;
-    __syncthreads();
-    if (threadIdx.x == 0) sm_carry += sm_warp[32];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) P.tile_prefix[P.B] = sm_carry;
-}
 
 // ------------------------------------------------------------------------------------------------
 // Softmax / epilogue of one segment, executed by the 128 threads of warps 0-3 (thread = TMEM lane).
@@ -708,7 +391,7 @@ attn_tc_kernel(const TcParams P, const __grid_constant__ CUtensorMap tmap_k, con
   if (P.B <= kMaxSmemPrefixSlots) {
     int* sm_prefix = reinterpret_cast<int*>(smem + kSmPrefix);
     int* sm_slot = reinterpret_cast<int*>(smem + kSmSlot);
-    block_tile_prefix(P, sm_prefix, sm_slot, reinterpret_cast<int*>(smem + kSmMl), cta == 0);
+    block_tile_prefix<kSegCost, kThreads>(P, sm_prefix, sm_slot, reinterpret_cast<int*>(smem + kSmMl), cta == 0);
     prefix = sm_prefix;
     slot_info = sm_slot;
   }
@@ -717,7 +400,7 @@ attn_tc_kernel(const TcParams P, const __grid_constant__ CUtensorMap tmap_k, con
   if (warp >= 4 && warp < 4 + kProducerWarps) {
     // =========================================================================== TMA producers
     const uint32_t pw = (uint32_t)(warp - 4);  // this warp serves the fills f with f % kProducerWarps == pw
-    WorkIter it;
+    WorkIter<kSegCost> it;
     it.init(P, cta, prefix, slot_info);
     Segment sg;
     uint32_t fill = 0;
@@ -779,7 +462,7 @@ attn_tc_kernel(const TcParams P, const __grid_constant__ CUtensorMap tmap_k, con
     }
   } else if (warp == 7) {
     // =========================================================================== MMA issuer
-    WorkIter it;
+    WorkIter<kSegCost> it;
     it.init(P, cta, prefix, slot_info);
     Segment sg;
     uint32_t cons = 0, n = 0, seg = 0;
@@ -847,7 +530,7 @@ attn_tc_kernel(const TcParams P, const __grid_constant__ CUtensorMap tmap_k, con
     }
   } else if (warp < 4) {
     // =========================================================================== softmax / epilogue
-    WorkIter it;
+    WorkIter<kSegCost> it;
     it.init(P, cta, prefix, slot_info);
     Segment sg;
     SoftmaxCtx sc;
@@ -877,102 +560,6 @@ attn_tc_kernel(const TcParams P, const __grid_constant__ CUtensorMap tmap_k, con
   if (warp == 4) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
-  }
-}
-
-// ------------------------------------------------------------------------------------------------
-// Combine: pairs whose tiles were split over several CTAs (log-sum-exp merge of the partials)
-// ------------------------------------------------------------------------------------------------
-// One CTA per share of the main kernel: CTA c merges the pair that starts inside share c and runs on
-// into later shares (every split pair has exactly one such share).  The kernel is pure latency (a few
-// dependent rounds of small loads), so it is laid out wide: the slot of the share's last tile is found by
-// a counting vote over the tile prefix instead of a binary search of dependent loads, and one warp per
-// block row merges all partials of its row in a single round.
-constexpr int kCombineThreads = 1024;
-__global__ void __launch_bounds__(kCombineThreads) attn_combine_kernel(const TcParams P) {
-  const int c0 = blockIdx.x;
-  pdl_wait();
-  pdl_launch_dependents();
-  const long long total = (long long)P.tile_prefix[P.B] * P.Hkv;
-  if (total == 0) return;
-  const long long per = share_units(total, P.num_ctas);
-  const long long t_last = ((long long)(c0 + 1) * per < total ? (long long)(c0 + 1) * per : total) - 1;
-  if (t_last < (long long)c0 * per) return;  // empty share
-  // slot of the share's last tile = number of slots whose tiles all lie at or before t_last
-  __shared__ int sm_cnt;
-  if (threadIdx.x == 0) sm_cnt = 0;
-  __syncthreads();
-  {
-    int cnt = 0;
-    for (int i = threadIdx.x; i < P.B; i += kCombineThreads)
-      cnt += ((long long)P.tile_prefix[i + 1] * P.Hkv <= t_last) ? 1 : 0;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) cnt += __shfl_xor_sync(0xffffffffu, cnt, off);
-    if ((threadIdx.x & 31) == 0 && cnt) atomicAdd(&sm_cnt, cnt);
-  }
-  __syncthreads();
-  const int b = sm_cnt;
-  const int T = P.tile_prefix[b + 1] - P.tile_prefix[b];  // on the split axis: kSegCost units, then the tiles
-  const int g = (int)((t_last - (long long)P.tile_prefix[b] * P.Hkv) / T);
-  const long long p0 = (long long)P.tile_prefix[b] * P.Hkv + (long long)g * T, p1 = p0 + T;
-  const int c_first = (int)((p0 + kSegCost) / per), c_last = (int)((p1 - 1) / per);  // shares that hold tiles of the pair
-  if (c_first != c0 || c_last == c0) return;  // merged by an earlier share, or written directly
-  const int q_len = P.n_ver[b] + P.N;
-  const int rows_valid = q_len * P.G;
-  // replicas of a row (key split across lane groups, see softmax_segment) are further partials
-  const int F = rows_valid > 64 ? 1 : (rows_valid > 32 ? 2 : 4);
-  const int RG = 128 / F;
-  const int lane = threadIdx.x & 31;
-  const int n_part = (c_last - c_first + 1) * F;  // partials of a row: lane i < n_part fetches the i-th (max, sum)
-  for (int row = threadIdx.x >> 5; row < rows_valid; row += kCombineThreads / 32) {
-    float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int base = 0; base < n_part; base += 32) {
-      // one round of loads for up to 32 partials: every lane reads one (max, sum) pair
-      float m_i = -INFINITY, l_i = 0.f;
-      size_t rr_i = 0;
-      if (base + lane < n_part) {
-        const int c = c_first + (base + lane) / F, pp = (base + lane) % F;
-        const int slot = c * 2 + (((long long)c * per >= p0) ? 0 : 1);
-        rr_i = (size_t)slot * 128 + pp * RG + row;
-        const float2 ml = *reinterpret_cast<const float2*>(P.part_ml + rr_i * 2);
-        m_i = ml.x;
-        l_i = ml.y;
-      }
-      float Mn = m_i;
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) Mn = fmaxf(Mn, __shfl_xor_sync(0xffffffffu, Mn, off));
-      Mn = fmaxf(Mn, M);
-      const float keep = (M == -INFINITY) ? 0.f : ex2f(M - Mn);
-      L *= keep;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] *= keep;
-      M = Mn;
-      const float w_i = (m_i == -INFINITY) ? 0.f : ex2f(m_i - M);
-      const int cnt = min(32, n_part - base);
-      for (int i = 0; i < cnt; i += 4) {  // four independent loads in flight
-        float4 o[4];
-        float w[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int ii = min(i + u, cnt - 1);
-          const float wu = __shfl_sync(0xffffffffu, w_i, ii);
-          const float lu = __shfl_sync(0xffffffffu, l_i, ii);
-          const size_t rr = __shfl_sync(0xffffffffu, (unsigned long long)rr_i, ii);
-          w[u] = (i + u < cnt) ? wu : 0.f;
-          L += lu * w[u];
-          o[u] = *reinterpret_cast<const float4*>(P.part_o + rr * 128 + lane * 4);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          acc[0] += o[u].x * w[u]; acc[1] += o[u].y * w[u]; acc[2] += o[u].z * w[u]; acc[3] += o[u].w * w[u];
-        }
-      }
-    }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
-    const int r = row / P.G, hg = row % P.G;
-    const size_t o_off = (((size_t)b * P.Q + r) * P.Hq + g * P.G + hg) * ISD_HEAD_DIM + lane * 4;
-    *reinterpret_cast<uint2*>(P.out + o_off) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
-    if (P.lse && lane == 0) P.lse[((size_t)b * P.Q + r) * P.Hq + g * P.G + hg] = (M + log2f(L)) * kLn2;
   }
 }
 
@@ -1087,12 +674,12 @@ int isd_launch_attn_tc(isd_ctx* ctx, const isd_batch_state* st, const void* q, c
   P.num_ctas = ctx->attn_ctas;
   P.wait_ns = ctx->wait_ns;
   cudaError_t e = cudaSuccess;
-  if (c.batch > kMaxSmemPrefixSlots) e = isd_launch_pdl(attn_plan_kernel, dim3(1), dim3(1024), 0, stream, P);
+  if (c.batch > kMaxSmemPrefixSlots) e = isd_launch_pdl(attn_plan_kernel<kSegCost>, dim3(1), dim3(1024), 0, stream, P);
   if (ctx->ev_attn0) cudaEventRecord(ctx->ev_attn0, stream);
   if (e == cudaSuccess)
     e = isd_launch_pdl(attn_tc_kernel, dim3(ctx->attn_ctas), dim3(kThreads), kSmemBytes, stream, P, pm->map_k, pm->map_v);
   if (ctx->ev_attn1) cudaEventRecord(ctx->ev_attn1, stream);
-  if (e == cudaSuccess) e = isd_launch_pdl(attn_combine_kernel, dim3(ctx->attn_ctas), dim3(kCombineThreads), 0, stream, P);
+  if (e == cudaSuccess) e = isd_launch_pdl(attn_combine_kernel<kSegCost, true>, dim3(ctx->attn_ctas), dim3(kCombineThreads), 0, stream, P);
   ctx->launches += 2 + (c.batch > kMaxSmemPrefixSlots ? 1 : 0);
   return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }
