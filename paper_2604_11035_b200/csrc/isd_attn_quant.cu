@@ -34,6 +34,7 @@ namespace {
 constexpr int kQuantThreads = 640;
 constexpr int kStageQ = 8 * kQTile;    // one tile of 128 keys: eight pages' tiles
 constexpr int kQuantSegCost = 4;       // fixed cost of a segment in units of one tile's time
+constexpr float kNoRef = 3.0e38f;      // any score plus this asks for a reference; a masked one (-inf) does not
 constexpr int kScaleBufs = 4;          // the K decoders run at most three tiles ahead of the softmax
 
 struct QuantParams : SplitParams {
@@ -56,10 +57,11 @@ struct Cfg {
   static constexpr int kSmRing = kSmP + 2 * (RMAX / 64) * 16384;
   static constexpr int kSmBar = kSmRing + kStages * kStageQ;
   static constexpr int kSmScale = kSmBar + 512;       // [kScaleBufs][128] x {sk * scale2, sv}
-  static constexpr int kSmNegM = kSmScale + kScaleBufs * 128 * 8;  // [128] -reference maximum per row (+inf: none yet)
+  static constexpr int kSmNegM = kSmScale + kScaleBufs * 128 * 8;  // [128] -reference maximum per row (kNoRef: none yet)
   static constexpr int kSmF = kSmNegM + 512;          // [128] factor of a raise
   static constexpr int kSmRed = kSmF + 512;           // [4 warps][128] warp results
-  static constexpr int kSmPrefix = kSmRed + 2048;
+  static constexpr int kSmSeg = kSmRed + 2048;         // ring of segments, 32 bytes each
+  static constexpr int kSmPrefix = kSmSeg + 128;
   static constexpr int kSmSlot = kSmPrefix + (kMaxSmemPrefixSlots + 1) * 4 + 12;
   static constexpr int kSmemBytes = kSmSlot + kMaxSmemPrefixSlots * 4;
   static constexpr uint32_t kTmK = 0, kTmV = kTmK + kA * 64, kTmS = kTmV + kA * 64, kTmO = kTmS + 2 * RMAX;
@@ -71,7 +73,7 @@ struct Cfg {
   enum {
     FULL = 0, EMPTY = FULL + kStages, KFULL = EMPTY + kStages, KFREE = KFULL + kA, VFULL = KFREE + kA, VFREE = VFULL + kA,
     SCALE = VFREE + kA, SFULL = SCALE + kScaleBufs, PFULL = SFULL + 2, ODONE = PFULL + 2, QFULL = ODONE + 2, QFREE = QFULL + 2,
-    OFREE = QFREE + 2, COUNT
+    OFREE = QFREE + 2, SEGFULL, SEGFREE = SEGFULL + 4, COUNT = SEGFREE + 4
   };
   static_assert(COUNT * 8 + 32 <= 512, "barrier block");
 };
@@ -117,10 +119,10 @@ __device__ __forceinline__ bool wg_any(int wg, bool v) {
                : "=r"(r) : "r"((uint32_t)v), "r"(1 + wg) : "memory");
   return r != 0;
 }
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
-  return x;
+__device__ __forceinline__ float warp_max(float x) {  // (a NaN is passed over)
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 struct Shared {  // what every role needs
@@ -130,6 +132,36 @@ struct Shared {  // what every role needs
   __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8u * (uint32_t)i; }
   __device__ __forceinline__ bool wait(int i, uint32_t parity) const { return mbar_wait(bar(i), parity & 1u, abort_flag); }
 };
+
+// The CTA's segments are worked out by one warp and handed to the other roles through a ring in shared memory: the
+// enumeration (64-bit divisions) would otherwise sit in every role's code, and the roles share one instruction cache.
+constexpr int kSegRing = 4;
+constexpr int kSegReaders = 19;  // warps
+template <class C>
+__device__ __forceinline__ bool take_segment(const Shared& S, uint32_t k, Segment& sg) {
+  const int i = (int)(k % kSegRing);
+  if (!S.wait(C::SEGFULL + i, k / kSegRing)) return false;
+  const int4* src = reinterpret_cast<const int4*>(S.smem + C::kSmSeg) + 2 * i;
+  const int4 a = src[0], b = src[1];
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(S.bar(C::SEGFREE + i));
+  sg.b = a.x; sg.g = a.y; sg.j0 = a.z; sg.j1 = a.w;
+  sg.ctx = b.x; sg.q_len = b.y; sg.part_slot = b.z;
+  sg.kv_len = sg.ctx + sg.q_len;
+  return a.x >= 0;  // a slot of -1 ends the list
+}
+template <class C>
+__device__ __forceinline__ bool give_segment(const Shared& S, uint32_t k, const Segment& sg) {
+  const int i = (int)(k % kSegRing);
+  if (!S.wait(C::SEGFREE + i, (k / kSegRing) ^ 1u)) return false;
+  if ((threadIdx.x & 31) == 0) {
+    int4* dst = reinterpret_cast<int4*>(S.smem + C::kSmSeg) + 2 * i;
+    dst[0] = make_int4(sg.b, sg.g, sg.j0, sg.j1);
+    dst[1] = make_int4(sg.ctx, sg.q_len, sg.part_slot, 0);
+    mbar_arrive(S.bar(C::SEGFULL + i));
+  }
+  return true;
+}
 
 // ------------------------------------------------------------------------------------------------
 // Softmax and epilogue of one segment by warpgroup wg (0, 1): rows [16 c0, 16 c1) of the block
@@ -150,7 +182,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
   uint64_t l2[C::kChunks * 8];  // row sums of this lane's keys, pairs of rows
 #pragma unroll
   for (int i = 0; i < C::kChunks * 8; ++i) l2[i] = 0;
-  if (tl < mine * 16) neg_m[tl] = INFINITY;
+  if (tl < mine * 16) neg_m[tl] = kNoRef;
   wg_sync(wg);
   bool ok = true;
   for (int i = 0; i < cnt; ++i) {
@@ -163,35 +195,43 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
     if (!ok) break;
     tc_fence_after();
     const uint2 scl = lds64(S.base + C::kSmScale + ((nn % kScaleBufs) * 128 + (uint32_t)tl) * 8);
-    const float sk = __uint_as_float(scl.x), sv = __uint_as_float(scl.y);
-    const uint64_t sk2 = pack2(sk, sk), sv2 = pack2(sv, sv);
+    float sk = __uint_as_float(scl.x), sv = __uint_as_float(scl.y);
     const uint32_t ts = S.tmem + C::kTmS + (nn & 1u) * RMAX + (uint32_t)c0 * 16 + lane_base;
-    // x = score (log2 domain) - reference of chunk c's 16 rows; -inf where the row does not see the key.  Returns their maximum.
+    // Tiles that reach into the block: the scores go back to tensor memory with -inf where the row does not see the key (and
+    // NaN where it does and the value scale is NaN, which then needs no factor), so that all other tiles are spared the masks.
+    if (edge && mine > 0) {
+      const bool bad_sv = sv != sv;
+#pragma unroll 1
+      for (int c = 0; c < mine; ++c) {
+        uint32_t raw[16];
+        TMEM_LD16(ts + c * 16, raw, 0);
+        tmem_wait_ld();
+        const float add = bad_sv ? sv : 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          raw[k] = (c0 + c) * 16 + k < vmin ? 0xFF800000u : __float_as_uint(fmaf(__uint_as_float(raw[k]), sk, add));
+        TMEM_ST16(ts + c * 16, raw, 0);
+      }
+      tmem_wait_st();
+      sk = 1.f;
+      if (bad_sv || vmin == 0x7FFFFFFF) sv = 0.f;
+    }
+    const uint64_t sk2 = pack2(sk, sk), sv2 = pack2(sv, sv);
+    // x = score (log2 domain) - reference of chunk c's 16 rows; returns their maximum
     auto arguments = [&](int c, const uint32_t* raw, uint64_t* x) -> float {
       float mx = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint4 nm = lds128(neg_m_a + c * 64 + k * 16);
-        uint64_t a = fma2(pack2(__uint_as_float(raw[4 * k]), __uint_as_float(raw[4 * k + 1])), sk2,
-                          pack2(__uint_as_float(nm.x), __uint_as_float(nm.y)));
-        uint64_t b = fma2(pack2(__uint_as_float(raw[4 * k + 2]), __uint_as_float(raw[4 * k + 3])), sk2,
-                          pack2(__uint_as_float(nm.z), __uint_as_float(nm.w)));
+        x[2 * k] = fma2(pack2(__uint_as_float(raw[4 * k]), __uint_as_float(raw[4 * k + 1])), sk2,
+                        pack2(__uint_as_float(nm.x), __uint_as_float(nm.y)));
+        x[2 * k + 1] = fma2(pack2(__uint_as_float(raw[4 * k + 2]), __uint_as_float(raw[4 * k + 3])), sk2,
+                            pack2(__uint_as_float(nm.z), __uint_as_float(nm.w)));
         float e0, e1, e2, e3;
-        unpack2(a, e0, e1);
-        unpack2(b, e2, e3);
-        if (edge) {
-          const int v = (c0 + c) * 16 + 4 * k;
-          if (v + 0 < vmin) e0 = -INFINITY;
-          if (v + 1 < vmin) e1 = -INFINITY;
-          if (v + 2 < vmin) e2 = -INFINITY;
-          if (v + 3 < vmin) e3 = -INFINITY;
-          a = pack2(e0, e1);
-          b = pack2(e2, e3);
-        }
+        unpack2(x[2 * k], e0, e1);
+        unpack2(x[2 * k + 1], e2, e3);
         mx = max3(mx, e0, e1);
         mx = max3(mx, e2, e3);
-        x[2 * k] = a;
-        x[2 * k + 1] = b;
       }
       return mx;
     };
@@ -220,8 +260,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
       return mx;
     };
     if (mine > 0) {
-      const bool grow = all_arguments() > 8.f;
-      if (wg_any(wg, grow)) {
+      for (int raised = 0; wg_any(wg, all_arguments() > 8.f) && !raised; ++raised) {
         // ---- raise the reference of this warpgroup's rows to the maximum so far (first tile, and when a score has grown
         // by more than 2^8): sums and O are scaled by 2^(old - new)
 #pragma unroll 1
@@ -231,17 +270,16 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
           tmem_wait_ld();
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            float s = __uint_as_float(raw[k]) * sk;
-            if (edge && (c0 + c) * 16 + k < vmin) s = -INFINITY;
-            s = warp_max(s);
+            const float s = warp_max(__uint_as_float(raw[k]) * sk);
             if (lane == 0) red[warp * 128 + c * 16 + k] = s;
           }
         }
         wg_sync(wg);
         if (tl < mine * 16) {
           const float old = -neg_m[tl];
-          const float m = fmaxf(fmaxf(fmaxf(red[tl], red[128 + tl]), fmaxf(red[256 + tl], red[384 + tl])), old);
-          fac[tl] = (old == -INFINITY || m == old) ? 1.f : ex2f(old - m);  // (no reference yet: sums and O are zero)
+          float m = fmaxf(fmaxf(red[tl], red[128 + tl]), fmaxf(red[256 + tl], red[384 + tl]));
+          m = fmaxf(fmaf(fabsf(m), 0x1p-22f, m), old);  // a little above, so that no rounding leaves a positive argument
+          fac[tl] = old == -kNoRef ? 1.f : ex2f(old - m);  // (no reference yet: sums and O are zero)
           neg_m[tl] = -m;
         }
         wg_sync(wg);
@@ -257,8 +295,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
           }
         if (i > 0) {
           // PV(nn - 1) must have finished before O is touched (two barriers: see the bf16 kernel)
-          ok = S.wait(C::ODONE + (int)((nn - 1u) & 1u), (nn - 1u) >> 1);
-          if (!ok) break;
+          if (!S.wait(C::ODONE + (int)((nn - 1u) & 1u), (nn - 1u) >> 1)) return false;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < mine; ++c) {
@@ -272,7 +309,6 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
           }
           tmem_wait_st();
         }
-        if (kKeep) all_arguments();
       }
       // ---- probabilities, row sums, and the operand sv * p (rows of a key are contiguous: MN-major, 128-byte swizzle)
       const uint32_t pb = S.base + C::kSmP + (nn & 1u) * (RMAX / 64) * 16384 + (uint32_t)tl * 128;
@@ -295,11 +331,6 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
             l2[c * 8 + k] = add2(l2[c * 8 + k], p);
             float pa, pc;
             unpack2(mul2(p, sv2), pa, pc);
-            if (edge) {  // a key the row does not see has no part, whatever its scale is
-              const int v = (c0 + c) * 16 + 2 * k;
-              if (v < vmin) pa = 0.f;
-              if (v + 1 < vmin) pc = 0.f;
-            }
             pk[k] = pack_bf16_cvt(pa, pc);
           }
           const int cc = c0 + c;
@@ -336,7 +367,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
   wg_sync(wg);
   if (tl < mine * 16) {
     const float l = (red[tl] + red[128 + tl]) + (red[256 + tl] + red[384 + tl]);
-    const float m = -neg_m[tl];
+    const float m = neg_m[tl] == kNoRef ? -INFINITY : -neg_m[tl];
     const int v = c0 * 16 + tl;
     fac[tl] = l == 0.f ? 0.f : 1.f / l;
     if (v < rows) {
@@ -409,6 +440,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
       mbar_init(S.bar(C::QFULL + i), 1); mbar_init(S.bar(C::QFREE + i), 1);
     }
     mbar_init(S.bar(C::OFREE), 8);
+    for (int i = 0; i < kSegRing; ++i) { mbar_init(S.bar(C::SEGFULL + i), 1); mbar_init(S.bar(C::SEGFREE + i), kSegReaders); }
     *S.abort_flag = (S.base & 1023u) ? 1 : 0;  // the swizzled layouts assume a 1 KiB aligned window
     *reinterpret_cast<volatile unsigned long long*>(S.abort_flag + 2) = P.wait_ns;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -437,8 +469,6 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     prefix = sm_prefix;
     slot_info = sm_slot;
   }
-  WorkIter<kQuantSegCost> it;
-  it.init(P, cta, prefix, slot_info);
   Segment sg;
   const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
 
@@ -449,32 +479,28 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     const int key = warp * 32 + lane;
     const uint32_t in_stage = (uint32_t)(key >> 4) * kQTile, t = (uint32_t)key & 15u;
     bool ok = true;
-    while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
       for (int j = sg.j0; j < sg.j1; ++j, ++n) {
         const uint32_t s = n % C::kStages, a = n % C::kA;
         ok = S.wait(C::FULL + (int)s, n / C::kStages);
         if (!ok) break;
         const uint32_t src = S.base + C::kSmRing + s * kStageQ + in_stage;
-        uint4 w[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) w[c] = lds128(src + c * 256 + t * 16);
         const uint32_t meta = src + kQOffMeta + t * 2;
         const float sk = __uint_as_float(lds_u16(meta) << 16) * P.scale2, sv = __uint_as_float(lds_u16(meta + 64) << 16);
         const uint32_t z = lds_u16(meta + 32) * 0x10001u;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(S.bar(C::EMPTY + (int)s));
         if (n >= (uint32_t)C::kA) ok = S.wait(C::KFREE + (int)a, n / C::kA - 1);
         if (!ok) break;
         tc_fence_after();
         // QK(n - 2) is done; it was issued after PV(n - 4), which waited until the softmax of tile n - 4 had read its scales
         asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(S.base + C::kSmScale + ((n % kScaleBufs) * 128 + (uint32_t)key) * 8), "f"(sk), "f"(sv) : "memory");
         const uint32_t tk = S.tmem + C::kTmK + a * 64 + lane_base;
-#pragma unroll
+#pragma unroll 1
         for (int h = 0; h < 2; ++h) {
           uint32_t o[32];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const uint32_t ww[4] = {w[2 * h + c].x, w[2 * h + c].y, w[2 * h + c].z, w[2 * h + c].w};
+            const uint4 w = lds128(src + (2 * h + c) * 256 + t * 16);
+            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -482,6 +508,8 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
           }
           TMEM_ST32(tk + h * 32, o, 0);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(S.bar(C::EMPTY + (int)s));
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -497,7 +525,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     uint32_t n = 0;
     const int dim = (warp & 3) * 32 + lane;
     bool ok = true;
-    while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
       for (int j = sg.j0; j < sg.j1; ++j, ++n) {
         const uint32_t s = n % C::kStages, a = n % C::kA;
         ok = S.wait(C::FULL + (int)s, n / C::kStages);
@@ -506,12 +534,12 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
         tc_fence_after();
         const uint32_t src = S.base + C::kSmRing + s * kStageQ;
         const uint32_t tv = S.tmem + C::kTmV + a * 64 + lane_base;
+#pragma unroll 1
+        for (int h = 0; h < 4; ++h) {
+          uint32_t o[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t o[32];
-#pragma unroll
-          for (int p = 0; p < 4; ++p) {
-            const uint32_t pg = src + (uint32_t)(h * 4 + p) * kQTile;
+          for (int p = 0; p < 2; ++p) {
+            const uint32_t pg = src + (uint32_t)(h * 2 + p) * kQTile;
             const uint2 w = lds64(pg + kQOffV + dim * 8);
             const uint4 z0 = lds128(pg + kQOffMeta + 96), z1 = lds128(pg + kQOffMeta + 112);
             const uint32_t z[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
@@ -521,7 +549,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
               o[p * 8 + 4 + e] = sub_zero(codes_to_bf16(w.y >> (4 * e)), z[4 + e]);
             }
           }
-          TMEM_ST32(tv + h * 32, o, 0);
+          TMEM_ST16(tv + h * 16, o, 0);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(S.bar(C::EMPTY + (int)s));
@@ -536,7 +564,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     regs_inc<C::kRegsSoftmax>();
     uint32_t n = 0;
     bool ok = true;
-    while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
       ok = softmax_segment_q<RMAX>(P, sg, S, (warp - 8) >> 2, n);
     }
   } else {
@@ -546,7 +574,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
       const uint32_t pw = warp == 16 ? 0u : 1u;
       uint32_t n = 0;
       bool ok = true;
-      while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+      for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
         const int32_t* pt = P.page_table + (size_t)sg.b * P.max_pages;
         const int total_pages = (sg.kv_len + ISD_PAGE - 1) / ISD_PAGE;
         // page ids 32 at a time (4 tiles), one chunk ahead
@@ -582,9 +610,9 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
       }
     } else if (warp == 17) {
       // ========================================================================= MMA issuer
-      uint32_t n = 0, seg = 0;
+      uint32_t n = 0;
       bool ok = true;
-      while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+      for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
         const int cnt = sg.j1 - sg.j0;
         const uint32_t ncols = (uint32_t)((sg.q_len * P.G + 15) & ~15);
         const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((ncols >> 3) << 17) | ((128u >> 4) << 24);
@@ -627,19 +655,23 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
           __syncwarp();
           return true;
         };
-        ok = qk(n, cnt == 1);
-        for (int i = 0; i < cnt && ok; ++i) {
+#pragma unroll 1
+        for (int i = -1; i < cnt && ok; ++i) {
           if (i + 1 < cnt) ok = qk(n + i + 1, i + 2 == cnt);
-          if (ok) ok = pv(n + i, i == 0);
+          if (ok && i >= 0) ok = pv(n + i, i == 0);
         }
         n += (uint32_t)cnt;
-        ++seg;
       }
     } else {
-      // ========================================================================= Q: rows of the block, a segment ahead
-      uint32_t seg = 0;
+      // ========================================================================= segments and their Q, a segment ahead
+      WorkIter<kQuantSegCost> it;
+      it.init(P, cta, prefix, slot_info);
       bool ok = true;
-      while (ok && it.next(P, cta, sg) && !*S.abort_flag) {
+      for (uint32_t seg = 0; ok; ++seg) {
+        const bool have = it.next(P, cta, sg);
+        if (!have) sg.b = -1;
+        ok = give_segment<C>(S, seg, sg);
+        if (!have || !ok) break;
         if (seg >= 2) ok = S.wait(C::QFREE + (int)(seg & 1u), (seg >> 1) - 1u);
         if (!ok) break;
         const int rows = sg.q_len * P.G, padded = (rows + 15) & ~15;
@@ -663,7 +695,6 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(S.bar(C::QFULL + (int)(seg & 1u)));
-        ++seg;
       }
     }
   }
