@@ -12,9 +12,9 @@
 // products for a block of at most 60 rows.  Here the KEYS are M and the rows are N (a multiple of 16):
 //     S^T[key, row] = K[key, :] Q^T           A = K  from tensor memory (lane = key),   B = Q from shared memory
 //     O^T[dim, row] += V^T[dim, key] P^T      A = V^T from tensor memory (lane = dim),  B = P from shared memory
-// so the tensor cores do the work the rows need, and the decoded tiles never touch shared memory: a thread of the decoding
-// warps owns a key (K) or a dim (V, which the cache stores dim-major within a page), turns its 64 bytes of codes into bf16
-// pairs (one LOP3 each: 128 + c; one subtraction: c - z) and stores them to its lane of tensor memory.
+// so the tensor cores do the work the rows need, and the decoded tiles never touch shared memory: a decoder thread owns a
+// key (K) or a dim (V, which the cache stores dim-major within a page), turns its 64 bytes of codes into bf16 pairs
+// (one LOP3: 128 + c; one subtraction: c - z) and stores them to its lane of tensor memory.
 //
 // Softmax.  A thread owns a key's lane and walks the rows: the running maximum would need a reduction over lanes per
 // tile.  It is replaced by a reference maximum per row that is only raised when some score passes it by more than 2^8
@@ -22,8 +22,8 @@
 // tile costs one vote of the warpgroup.  Row sums stay in registers per lane and are reduced over lanes once a segment.
 //
 // Warps: 0-3 decode K, 4-7 decode V, 8-11 and 12-15 softmax and epilogue of one half of the rows each, 16 and 18 copy pages
-// (one bulk copy of 2176 bytes holds K and V of a (page, head)), 17 issues the MMAs, 19 stages Q.  Work split and combine
-// pass: isd_attn_split.cuh.  Every wait is bounded, as in the bf16 kernel.
+// (one bulk copy of 2176 bytes holds K and V of a (page, head)), 17 issues the MMAs, 19 works out the CTA's segments and
+// stages their Q.  Work split and combine pass: isd_attn_split.cuh.  Every wait is bounded, as in the bf16 kernel.
 #include <new>
 
 #include "isd_attn_split.cuh"
@@ -35,7 +35,9 @@ constexpr int kQuantThreads = 640;
 constexpr int kStageQ = 8 * kQTile;    // one tile of 128 keys: eight pages' tiles
 constexpr int kQuantSegCost = 4;       // fixed cost of a segment in units of one tile's time
 constexpr float kNoRef = 3.0e38f;      // any score plus this asks for a reference; a masked one (-inf) does not
-constexpr int kScaleBufs = 4;          // the K decoders run at most three tiles ahead of the softmax
+constexpr int kScaleBufs = 4;          // the decoders run at most three tiles ahead of the softmax
+constexpr int kSegRing = 4;
+constexpr int kSegReaders = 19;        // warps
 
 struct QuantParams : SplitParams {
   int max_pages, num_pages;
@@ -52,40 +54,43 @@ template <int RMAX>
 struct Cfg {
   static constexpr int kStages = RMAX == 64 ? 8 : 4;
   static constexpr int kA = RMAX == 64 ? 2 : 1;       // buffers of the decoded K and V tiles (64 columns each)
+  static constexpr int kChunks = RMAX / 32;           // chunks of 16 rows of a softmax warpgroup, at most
+  static constexpr int kCols = kChunks * 16;
   static constexpr int kSmQ = 0;                      // [2 segments][2 halves of d][RMAX rows][128 B], 128-byte swizzle
   static constexpr int kSmP = kSmQ + 2 * RMAX * 256;  // [2 tiles][RMAX / 64 halves of rows][128 keys][128 B], 128-byte swizzle
-  static constexpr int kSmRing = kSmP + 2 * (RMAX / 64) * 16384;
+  static constexpr int kPBytes = RMAX / 64 * 16384;
+  static constexpr int kSmRing = kSmP + 2 * kPBytes;
   static constexpr int kSmBar = kSmRing + kStages * kStageQ;
   static constexpr int kSmScale = kSmBar + 512;       // [kScaleBufs][128] x {sk * scale2, sv}
-  static constexpr int kSmNegM = kSmScale + kScaleBufs * 128 * 8;  // [128] -reference maximum per row (kNoRef: none yet)
-  static constexpr int kSmF = kSmNegM + 512;          // [128] factor of a raise
-  static constexpr int kSmRed = kSmF + 512;           // [4 warps][128] warp results
+  static constexpr int kSmNegM = kSmScale + kScaleBufs * 128 * 8;  // [2 warpgroups][64] -reference maximum per row (kNoRef: none yet)
+  static constexpr int kSmF = kSmNegM + 512;          // [2 warpgroups][64] factor of a raise, of the epilogue
+  static constexpr int kSmRed = kSmF + 512;           // [2 warpgroups][4 warps][64] warp results
   static constexpr int kSmSeg = kSmRed + 2048;         // ring of segments, 32 bytes each
   static constexpr int kSmPrefix = kSmSeg + 128;
   static constexpr int kSmSlot = kSmPrefix + (kMaxSmemPrefixSlots + 1) * 4 + 12;
   static constexpr int kSmemBytes = kSmSlot + kMaxSmemPrefixSlots * 4;
   static constexpr uint32_t kTmK = 0, kTmV = kTmK + kA * 64, kTmS = kTmV + kA * 64, kTmO = kTmS + 2 * RMAX;
-  static constexpr int kChunks = RMAX / 32;           // chunks of 16 rows of a softmax warpgroup
-  static constexpr int kRegsSoftmax = RMAX == 64 ? 136 : 144, kRegsDecode = 72, kRegsRest = RMAX == 64 ? 64 : 48;
   static_assert(kTmO + RMAX <= 512 && kSmemBytes <= 232448, "tensor memory / shared memory");
-  // 640 threads are launched with 96 registers each
-  static_assert(2 * 128 * kRegsSoftmax + 2 * 128 * kRegsDecode + 128 * kRegsRest <= 640 * 96, "register split");
   enum {
-    FULL = 0, EMPTY = FULL + kStages, KFULL = EMPTY + kStages, KFREE = KFULL + kA, VFULL = KFREE + kA, VFREE = VFULL + kA,
-    SCALE = VFREE + kA, SFULL = SCALE + kScaleBufs, PFULL = SFULL + 2, ODONE = PFULL + 2, QFULL = ODONE + 2, QFREE = QFULL + 2,
-    OFREE = QFREE + 2, SEGFULL, SEGFREE = SEGFULL + 4, COUNT = SEGFREE + 4
+    FULL = 0, EMPTY = FULL + kStages, KFULL = EMPTY + kStages, VFULL = KFULL + kA, SCALE = VFULL + kA, SFULL = SCALE + kScaleBufs, PFULL = SFULL + 2,
+    ODONE = PFULL + 2, QFULL = ODONE + 2, QFREE = QFULL + 2, OFREE = QFREE + 2, SEGFULL, SEGFREE = SEGFULL + 4, COUNT = SEGFREE + 4
   };
   static_assert(COUNT * 8 + 32 <= 512, "barrier block");
+  // Registers a thread: 640 threads are launched with 96 each and share them out anew.
+  static constexpr int kRegsSoftmax = RMAX == 64 ? 136 : 144, kRegsDecode = 72, kRegsRest = RMAX == 64 ? 64 : 48;
+  static_assert(2 * 128 * kRegsSoftmax + 2 * 128 * kRegsDecode + 128 * kRegsRest <= kQuantThreads * 96, "register split");
 };
 
-#define TMEM_LD16(taddr, v, o)                                                                          \
-  asm volatile(                                                                                         \
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "                                                         \
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"                                 \
-      : "=r"(v[o + 0]), "=r"(v[o + 1]), "=r"(v[o + 2]), "=r"(v[o + 3]), "=r"(v[o + 4]), "=r"(v[o + 5]), \
-        "=r"(v[o + 6]), "=r"(v[o + 7]), "=r"(v[o + 8]), "=r"(v[o + 9]), "=r"(v[o + 10]),                \
-        "=r"(v[o + 11]), "=r"(v[o + 12]), "=r"(v[o + 13]), "=r"(v[o + 14]), "=r"(v[o + 15])             \
-      : "r"(taddr))
+// 16 columns of the thread's lane, arrived (load and wait in one statement: what uses the registers cannot be moved between)
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
 
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
@@ -105,14 +110,11 @@ __device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ uint64_t pack2_bits(uint32_t a, uint32_t b) { return pack2(__uint_as_float(a), __uint_as_float(b)); }
 
 __device__ __forceinline__ void wg_sync(int wg) { asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
+template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ bool wg_any(int wg, bool v) {
   uint32_t r;
   asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbar.red.or.pred q, %2, 128, p;\nselp.u32 %0, 1, 0, q;\n}"
@@ -125,21 +127,43 @@ __device__ __forceinline__ float warp_max(float x) {  // (a NaN is passed over)
   return y;
 }
 
+// mbarrier probe that lets the hardware suspend the warp for up to 20 us
+__device__ __forceinline__ bool mbar_try_wait_long(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\n"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+      "selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+  return ok != 0;
+}
+
 struct Shared {  // what every role needs
   uint8_t* smem;
   uint32_t base, bar0, tmem;
   volatile int* abort_flag;
-  __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8u * (uint32_t)i; }
-  __device__ __forceinline__ bool wait(int i, uint32_t parity) const { return mbar_wait(bar(i), parity & 1u, abort_flag); }
+  __device__ __forceinline__ uint32_t bar(uint32_t i) const { return bar0 + 8u * i; }
+  __device__ __forceinline__ bool wait(uint32_t i, uint32_t parity) const {
+    if (mbar_try_wait_long(bar(i), parity & 1u)) return true;
+    unsigned long long t0 = 0;  // (at most one more suspension after another thread has given up)
+    while (!mbar_try_wait_long(bar(i), parity & 1u)) {
+      const unsigned long long now = isd_now_ns();
+      if (t0 == 0) t0 = now;
+      if (*abort_flag) return false;
+      if (now - t0 > *reinterpret_cast<const volatile unsigned long long*>(abort_flag + 2)) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+    return true;
+  }
 };
 
 // The CTA's segments are worked out by one warp and handed to the other roles through a ring in shared memory: the
 // enumeration (64-bit divisions) would otherwise sit in every role's code, and the roles share one instruction cache.
-constexpr int kSegRing = 4;
-constexpr int kSegReaders = 19;  // warps
 template <class C>
 __device__ __forceinline__ bool take_segment(const Shared& S, uint32_t k, Segment& sg) {
-  const int i = (int)(k % kSegRing);
+  const uint32_t i = k % kSegRing;
   if (!S.wait(C::SEGFULL + i, k / kSegRing)) return false;
   const int4* src = reinterpret_cast<const int4*>(S.smem + C::kSmSeg) + 2 * i;
   const int4 a = src[0], b = src[1];
@@ -152,7 +176,7 @@ __device__ __forceinline__ bool take_segment(const Shared& S, uint32_t k, Segmen
 }
 template <class C>
 __device__ __forceinline__ bool give_segment(const Shared& S, uint32_t k, const Segment& sg) {
-  const int i = (int)(k % kSegRing);
+  const uint32_t i = k % kSegRing;
   if (!S.wait(C::SEGFREE + i, (k / kSegRing) ^ 1u)) return false;
   if ((threadIdx.x & 31) == 0) {
     int4* dst = reinterpret_cast<int4*>(S.smem + C::kSmSeg) + 2 * i;
@@ -164,120 +188,101 @@ __device__ __forceinline__ bool give_segment(const Shared& S, uint32_t k, const 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Softmax and epilogue of one segment by warpgroup wg (0, 1): rows [16 c0, 16 c1) of the block
+// Softmax and epilogue of one segment by warpgroup wg (0, 1), which has half of the block's chunks of 16 rows
 // ------------------------------------------------------------------------------------------------
 template <int RMAX>
 __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Segment& sg, const Shared& S, int wg, uint32_t& n) {
   using C = Cfg<RMAX>;
+  constexpr bool kKeep = C::kChunks <= 2;  // arguments stay in registers between the vote and the exponentials
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, tl = warp * 32 + lane;  // tl: TMEM lane = key of the tile = dim of O
   const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
   const int rows = sg.q_len * P.G, chunks = (rows + 15) >> 4;
-  const int c0 = wg == 0 ? 0 : (chunks + 1) >> 1, c1 = wg == 0 ? (chunks + 1) >> 1 : chunks, mine = c1 - c0;
+  const int c0 = wg == 0 ? 0 : (chunks + 1) >> 1, mine = wg == 0 ? (chunks + 1) >> 1 : chunks >> 1;
   const int cnt = sg.j1 - sg.j0;
-  // the warpgroup's own half of each array (the two may be in different segments)
   float* neg_m = reinterpret_cast<float*>(S.smem + C::kSmNegM) + wg * 64;
   float* fac = reinterpret_cast<float*>(S.smem + C::kSmF) + wg * 64;
-  float* red = reinterpret_cast<float*>(S.smem + C::kSmRed) + wg * 64;  // [warp][128]
+  float* red = reinterpret_cast<float*>(S.smem + C::kSmRed) + wg * 256;  // [warp][64]
   const uint32_t neg_m_a = S.base + C::kSmNegM + wg * 256, fac_a = S.base + C::kSmF + wg * 256;
   uint64_t l2[C::kChunks * 8];  // row sums of this lane's keys, pairs of rows
 #pragma unroll
   for (int i = 0; i < C::kChunks * 8; ++i) l2[i] = 0;
-  if (tl < mine * 16) neg_m[tl] = kNoRef;
+  if (tl < C::kCols) neg_m[tl] = kNoRef;
   wg_sync(wg);
-  bool ok = true;
+  const uint32_t to = S.tmem + C::kTmO + (uint32_t)c0 * 16 + lane_base;
+  const uint32_t sw = ((uint32_t)tl & 7u) << 4, p_row = S.base + C::kSmP + (uint32_t)tl * 128;
   for (int i = 0; i < cnt; ++i) {
-    const uint32_t nn = n + (uint32_t)i;
-    const int key = (sg.j0 + i) * kTile + tl;
-    // rows v < vmin do not see this lane's key (row v of the packed block is block row v / G)
-    const bool edge = (sg.j0 + i + 1) * kTile > sg.ctx;
-    const int vmin = key >= sg.kv_len ? 0x7FFFFFFF : (key > sg.ctx ? (key - sg.ctx) * P.G : 0);
-    ok = S.wait(C::SFULL + (int)(nn & 1u), nn >> 1) && S.wait(C::SCALE + (int)(nn % kScaleBufs), nn / kScaleBufs);
-    if (!ok) break;
-    tc_fence_after();
+    const uint32_t nn = n + (uint32_t)i, buf = nn & 1u;
+    if (!S.wait(C::SCALE + nn % kScaleBufs, nn / kScaleBufs)) return false;
     const uint2 scl = lds64(S.base + C::kSmScale + ((nn % kScaleBufs) * 128 + (uint32_t)tl) * 8);
     float sk = __uint_as_float(scl.x), sv = __uint_as_float(scl.y);
-    const uint32_t ts = S.tmem + C::kTmS + (nn & 1u) * RMAX + (uint32_t)c0 * 16 + lane_base;
-    // Tiles that reach into the block: the scores go back to tensor memory with -inf where the row does not see the key (and
-    // NaN where it does and the value scale is NaN, which then needs no factor), so that all other tiles are spared the masks.
-    if (edge && mine > 0) {
-      const bool bad_sv = sv != sv;
-#pragma unroll 1
-      for (int c = 0; c < mine; ++c) {
-        uint32_t raw[16];
-        TMEM_LD16(ts + c * 16, raw, 0);
-        tmem_wait_ld();
+    if (!S.wait(C::SFULL + buf, nn >> 1)) return false;
+    if (mine > 0) {
+      tc_fence_after();
+      const uint32_t ts = S.tmem + C::kTmS + buf * RMAX + (uint32_t)c0 * 16 + lane_base;
+      // Tiles that reach into the block: the scores go back to tensor memory with -inf where the row does not see the key (and
+      // NaN where it does and the value scale is NaN, which then needs no factor), so that all other tiles are spared the masks.
+      if ((sg.j0 + i + 1) * kTile > sg.ctx) {
+        // rows v < vmin do not see this lane's key (row v of the packed block is block row v / G)
+        const int key = (sg.j0 + i) * kTile + tl;
+        const int vmin = key >= sg.kv_len ? 0x7FFFFFFF : (key > sg.ctx ? (key - sg.ctx) * P.G : 0);
+        const bool bad_sv = sv != sv;
         const float add = bad_sv ? sv : 0.f;
+#pragma unroll 1
+        for (int c = 0; c < mine; ++c) {
+          uint32_t raw[16];
+          tmem_ld16(ts + c * 16, raw);
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
-          raw[k] = (c0 + c) * 16 + k < vmin ? 0xFF800000u : __float_as_uint(fmaf(__uint_as_float(raw[k]), sk, add));
-        TMEM_ST16(ts + c * 16, raw, 0);
+          for (int k = 0; k < 16; ++k)
+            raw[k] = (c0 + c) * 16 + k < vmin ? 0xFF800000u : __float_as_uint(fmaf(__uint_as_float(raw[k]), sk, add));
+          TMEM_ST16(ts + c * 16, raw, 0);
+        }
+        tmem_wait_st();
+        sk = 1.f;
+        if (bad_sv || vmin == 0x7FFFFFFF) sv = 0.f;
       }
-      tmem_wait_st();
-      sk = 1.f;
-      if (bad_sv || vmin == 0x7FFFFFFF) sv = 0.f;
-    }
-    const uint64_t sk2 = pack2(sk, sk), sv2 = pack2(sv, sv);
-    // x = score (log2 domain) - reference of chunk c's 16 rows; returns their maximum
-    auto arguments = [&](int c, const uint32_t* raw, uint64_t* x) -> float {
-      float mx = -INFINITY;
+      const uint64_t sk2 = pack2(sk, sk), sv2 = pack2(sv, sv);
+      // ---- arguments x = score (log2 domain) - reference; does any pass 8?
+      uint64_t x2[kKeep ? C::kChunks * 8 : 8];
+      auto arguments = [&](int c, uint64_t* x) -> float {
+        uint32_t raw[16];
+        const uint4 m0 = lds128(neg_m_a + c * 64), m1 = lds128(neg_m_a + c * 64 + 16), m2 = lds128(neg_m_a + c * 64 + 32), m3 = lds128(neg_m_a + c * 64 + 48);
+        tmem_ld16(ts + c * 16, raw);
+        x[0] = fma2(pack2_bits(raw[0], raw[1]), sk2, pack2_bits(m0.x, m0.y));
+        x[1] = fma2(pack2_bits(raw[2], raw[3]), sk2, pack2_bits(m0.z, m0.w));
+        x[2] = fma2(pack2_bits(raw[4], raw[5]), sk2, pack2_bits(m1.x, m1.y));
+        x[3] = fma2(pack2_bits(raw[6], raw[7]), sk2, pack2_bits(m1.z, m1.w));
+        x[4] = fma2(pack2_bits(raw[8], raw[9]), sk2, pack2_bits(m2.x, m2.y));
+        x[5] = fma2(pack2_bits(raw[10], raw[11]), sk2, pack2_bits(m2.z, m2.w));
+        x[6] = fma2(pack2_bits(raw[12], raw[13]), sk2, pack2_bits(m3.x, m3.y));
+        x[7] = fma2(pack2_bits(raw[14], raw[15]), sk2, pack2_bits(m3.z, m3.w));
+        float a[8], b[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint4 nm = lds128(neg_m_a + c * 64 + k * 16);
-        x[2 * k] = fma2(pack2(__uint_as_float(raw[4 * k]), __uint_as_float(raw[4 * k + 1])), sk2,
-                        pack2(__uint_as_float(nm.x), __uint_as_float(nm.y)));
-        x[2 * k + 1] = fma2(pack2(__uint_as_float(raw[4 * k + 2]), __uint_as_float(raw[4 * k + 3])), sk2,
-                            pack2(__uint_as_float(nm.z), __uint_as_float(nm.w)));
-        float e0, e1, e2, e3;
-        unpack2(x[2 * k], e0, e1);
-        unpack2(x[2 * k + 1], e2, e3);
-        mx = max3(mx, e0, e1);
-        mx = max3(mx, e2, e3);
-      }
-      return mx;
-    };
-    // With at most 64 rows the arguments of the whole tile stay in registers between the vote and the exponentials; with
-    // 128 they would not fit beside the row sums, and the scores are read from tensor memory a second time.
-    constexpr bool kKeep = C::kChunks <= 2;
-    uint64_t x2[kKeep ? C::kChunks * 8 : 8];
-    auto all_arguments = [&]() -> float {
-      float mx = -INFINITY;
-      uint32_t raw[kKeep ? C::kChunks * 16 : 16];
-      if (kKeep) {
+        for (int k = 0; k < 8; ++k) unpack2(x[k], a[k], b[k]);
+        return fmaxf(max3(max3(a[0], b[0], a[1]), max3(b[1], a[2], b[2]), max3(a[3], b[3], a[4])),
+                     max3(max3(b[4], a[5], b[5]), max3(a[6], b[6], a[7]), b[7]));
+      };
+      for (int raised = 0;; ++raised) {
+        float mx = -INFINITY;
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c)
-          if (c < mine) TMEM_LD16(ts + c * 16, raw, (kKeep ? c * 16 : 0));
-        tmem_wait_ld();
-      }
-#pragma unroll
-      for (int c = 0; c < C::kChunks; ++c)
-        if (c < mine) {
-          if (!kKeep) {
-            TMEM_LD16(ts + c * 16, raw, 0);
-            tmem_wait_ld();
-          }
-          mx = fmaxf(mx, arguments(c, raw + (kKeep ? c * 16 : 0), x2 + (kKeep ? c * 8 : 0)));
-        }
-      return mx;
-    };
-    if (mine > 0) {
-      for (int raised = 0; wg_any(wg, all_arguments() > 8.f) && !raised; ++raised) {
+          if (c < mine) mx = fmaxf(mx, arguments(c, x2 + (kKeep ? c * 8 : 0)));
+        if (raised || !wg_any(wg, mx > 8.f)) break;
         // ---- raise the reference of this warpgroup's rows to the maximum so far (first tile, and when a score has grown
         // by more than 2^8): sums and O are scaled by 2^(old - new)
 #pragma unroll 1
         for (int c = 0; c < mine; ++c) {
           uint32_t raw[16];
-          TMEM_LD16(ts + c * 16, raw, 0);
-          tmem_wait_ld();
+          tmem_ld16(ts + c * 16, raw);
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
             const float s = warp_max(__uint_as_float(raw[k]) * sk);
-            if (lane == 0) red[warp * 128 + c * 16 + k] = s;
+            if (lane == 0) red[warp * 64 + c * 16 + k] = s;
           }
         }
         wg_sync(wg);
         if (tl < mine * 16) {
           const float old = -neg_m[tl];
-          float m = fmaxf(fmaxf(red[tl], red[128 + tl]), fmaxf(red[256 + tl], red[384 + tl]));
+          float m = fmaxf(fmaxf(red[tl], red[64 + tl]), fmaxf(red[128 + tl], red[192 + tl]));
           m = fmaxf(fmaf(fabsf(m), 0x1p-22f, m), old);  // a little above, so that no rounding leaves a positive argument
           fac[tl] = old == -kNoRef ? 1.f : ex2f(old - m);  // (no reference yet: sums and O are zero)
           neg_m[tl] = -m;
@@ -289,39 +294,31 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               const uint4 f = lds128(fac_a + c * 64 + k * 16);
-              l2[c * 8 + 2 * k] = mul2(l2[c * 8 + 2 * k], pack2(__uint_as_float(f.x), __uint_as_float(f.y)));
-              l2[c * 8 + 2 * k + 1] = mul2(l2[c * 8 + 2 * k + 1], pack2(__uint_as_float(f.z), __uint_as_float(f.w)));
+              l2[c * 8 + 2 * k] = mul2(l2[c * 8 + 2 * k], pack2_bits(f.x, f.y));
+              l2[c * 8 + 2 * k + 1] = mul2(l2[c * 8 + 2 * k + 1], pack2_bits(f.z, f.w));
             }
           }
         if (i > 0) {
           // PV(nn - 1) must have finished before O is touched (two barriers: see the bf16 kernel)
-          if (!S.wait(C::ODONE + (int)((nn - 1u) & 1u), (nn - 1u) >> 1)) return false;
+          if (!S.wait(C::ODONE + (buf ^ 1u), (nn - 1u) >> 1)) return false;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < mine; ++c) {
             uint32_t ov[16];
-            const uint32_t to = S.tmem + C::kTmO + (uint32_t)(c0 + c) * 16 + lane_base;
-            TMEM_LD16(to, ov, 0);
-            tmem_wait_ld();
+            tmem_ld16(to + c * 16, ov);
 #pragma unroll
             for (int k = 0; k < 16; ++k) ov[k] = __float_as_uint(__uint_as_float(ov[k]) * fac[c * 16 + k]);
-            TMEM_ST16(to, ov, 0);
+            TMEM_ST16(to + c * 16, ov, 0);
           }
           tmem_wait_st();
         }
       }
       // ---- probabilities, row sums, and the operand sv * p (rows of a key are contiguous: MN-major, 128-byte swizzle)
-      const uint32_t pb = S.base + C::kSmP + (nn & 1u) * (RMAX / 64) * 16384 + (uint32_t)tl * 128;
 #pragma unroll
-      for (int c = 0; c < C::kChunks; ++c) {
+      for (int c = 0; c < C::kChunks; ++c)
         if (c < mine) {
           uint64_t* x = x2 + (kKeep ? c * 8 : 0);
-          if (!kKeep) {
-            uint32_t raw[16];
-            TMEM_LD16(ts + c * 16, raw, 0);
-            tmem_wait_ld();
-            arguments(c, raw, x);
-          }
+          if (!kKeep) arguments(c, x);
           uint32_t pk[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
@@ -329,24 +326,20 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
             unpack2(x[k], a, b);
             const uint64_t p = pack2(ex2f(a), ex2f(b));
             l2[c * 8 + k] = add2(l2[c * 8 + k], p);
-            float pa, pc;
-            unpack2(mul2(p, sv2), pa, pc);
-            pk[k] = pack_bf16_cvt(pa, pc);
+            unpack2(mul2(p, sv2), a, b);
+            pk[k] = pack_bf16_cvt(a, b);
           }
           const int cc = c0 + c;
-          const uint32_t row = pb + (uint32_t)(cc >> 2) * 16384;
-          const uint32_t u = (uint32_t)(cc & 3) * 2, sw = (uint32_t)tl & 7u;
-          sts128(row + ((u ^ sw) << 4), pk[0], pk[1], pk[2], pk[3]);
-          sts128(row + (((u + 1) ^ sw) << 4), pk[4], pk[5], pk[6], pk[7]);
+          const uint32_t row = p_row + buf * C::kPBytes + (uint32_t)(cc >> 2) * 16384, u = (uint32_t)(cc & 3) * 32;
+          sts128(row + (u ^ sw), pk[0], pk[1], pk[2], pk[3]);
+          sts128(row + ((u + 16) ^ sw), pk[4], pk[5], pk[6], pk[7]);
         }
-      }
       fence_async_smem();
       tc_fence_before();
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(S.bar(C::PFULL + (int)(nn & 1u)));
+    if (lane == 0) mbar_arrive(S.bar(C::PFULL + buf));
   }
-  if (!ok) return false;
   // ---- row sums over the lanes: exchange halves until lane k of a warp holds the sum of row k of a 32-row group
 #pragma unroll
   for (int h = 0; h < (C::kChunks + 1) / 2; ++h) {
@@ -362,36 +355,33 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
         v[k] = keep + __shfl_xor_sync(0xffffffffu, give, off);
       }
     }
-    if (h * 32 + lane < mine * 16) red[warp * 128 + h * 32 + lane] = v[0];
+    red[warp * 64 + h * 32 + lane] = v[0];
   }
   wg_sync(wg);
   if (tl < mine * 16) {
-    const float l = (red[tl] + red[128 + tl]) + (red[256 + tl] + red[384 + tl]);
-    const float m = neg_m[tl] == kNoRef ? -INFINITY : -neg_m[tl];
+    const float L = (red[tl] + red[64 + tl]) + (red[128 + tl] + red[192 + tl]);
+    const float M = neg_m[tl] == kNoRef ? -INFINITY : -neg_m[tl];
     const int v = c0 * 16 + tl;
-    fac[tl] = l == 0.f ? 0.f : 1.f / l;
+    fac[tl] = L == 0.f ? 0.f : 1.f / L;
     if (v < rows) {
       if (sg.part_slot >= 0) {
-        // a row of NaN scores never got a reference: let the combine pass see it
-        P.part_ml[((size_t)sg.part_slot * 128 + v) * 2] = l == l ? m : INFINITY;
-        P.part_ml[((size_t)sg.part_slot * 128 + v) * 2 + 1] = l;
+        // (a row of NaN scores has no reference: let the combine pass see the NaN)
+        P.part_ml[((size_t)sg.part_slot * 128 + v) * 2] = L == L ? M : INFINITY;
+        P.part_ml[((size_t)sg.part_slot * 128 + v) * 2 + 1] = L;
       } else if (P.lse) {
-        P.lse[((size_t)sg.b * P.Q + v / P.G) * P.Hq + sg.g * P.G + v % P.G] = (m + log2f(l)) * kLn2;
+        P.lse[((size_t)sg.b * P.Q + v / P.G) * P.Hq + sg.g * P.G + v % P.G] = (M + log2f(L)) * kLn2;
       }
     }
   }
   wg_sync(wg);
   // ---- O: thread = dim, a column per row
   const uint32_t last = n + (uint32_t)cnt - 1;
-  ok = S.wait(C::ODONE + (int)(last & 1u), last >> 1);
-  if (!ok) return false;
+  if (!S.wait(C::ODONE + (last & 1u), last >> 1)) return false;
   tc_fence_after();
-  const uint32_t to = S.tmem + C::kTmO + (uint32_t)c0 * 16 + lane_base;
 #pragma unroll 1
   for (int c = 0; c < mine; ++c) {
     uint32_t ov[16];
-    TMEM_LD16(to + c * 16, ov, 0);
-    tmem_wait_ld();
+    tmem_ld16(to + c * 16, ov);
     const int v0 = (c0 + c) * 16;
     if (sg.part_slot >= 0) {
       float* dst = P.part_o + ((size_t)sg.part_slot * 128 + v0) * 128 + tl;
@@ -400,11 +390,13 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
         if (v0 + k < rows) dst[k * 128] = __uint_as_float(ov[k]);
     } else {
       int r = v0 / P.G, hg = v0 - r * P.G;
-      __nv_bfloat16* dst = P.out + ((size_t)sg.b * P.Q * P.Hq + sg.g * P.G) * ISD_HEAD_DIM + tl;
+      __nv_bfloat16* dst = P.out + (((size_t)sg.b * P.Q + r) * P.Hq + sg.g * P.G + hg) * ISD_HEAD_DIM + tl;
+      const int skip = (P.Hq - P.G) * ISD_HEAD_DIM;
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
-        if (v0 + k < rows) dst[((size_t)r * P.Hq + hg) * ISD_HEAD_DIM] = __float2bfloat16_rn(__uint_as_float(ov[k]) * fac[c * 16 + k]);
-        if (++hg == P.G) { hg = 0; ++r; }
+        if (v0 + k < rows) *dst = __float2bfloat16_rn(__uint_as_float(ov[k]) * fac[c * 16 + k]);
+        dst += ISD_HEAD_DIM;
+        if (++hg == P.G) { hg = 0; dst += skip; }
       }
     }
   }
@@ -413,6 +405,26 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
   if (lane == 0) mbar_arrive(S.bar(C::OFREE));
   n += (uint32_t)cnt;
   return true;
+}
+
+// One tile's QK^T into S[BUF] (eight steps of 16 dims), one tile's PV into O (eight steps of 16 keys).  Everything but the
+// query buffer and the number of rows is a constant.
+template <int RMAX, int BUF>
+__device__ __forceinline__ void issue_qk(const Shared& S, uint64_t q_desc, uint32_t idesc) {
+  using C = Cfg<RMAX>;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    tc_mma_ts(C::kTmS + BUF * RMAX, C::kTmK + (BUF % C::kA) * 64 + k * 8, q_desc + (uint64_t)((k >> 2) * (RMAX * 128 / 16) + (k & 3) * 2), idesc, k > 0);
+  tc_commit(S.bar(C::SFULL + BUF));
+}
+template <int RMAX, int BUF>
+__device__ __forceinline__ void issue_pv(const Shared& S, uint32_t idesc, bool accumulate) {
+  using C = Cfg<RMAX>;
+  const uint64_t p_desc = smem_desc(S.base + C::kSmP + BUF * C::kPBytes, 16384, 1024);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    tc_mma_ts(C::kTmO, C::kTmV + (BUF % C::kA) * 64 + k * 8, p_desc + (uint64_t)(k * 128), idesc, accumulate || k > 0);
+  tc_commit(S.bar(C::ODONE + BUF));
 }
 
 template <int RMAX>
@@ -430,10 +442,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
   // ---- set-up that touches nothing an earlier kernel wrote
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) { mbar_init(S.bar(C::FULL + i), 1); mbar_init(S.bar(C::EMPTY + i), 8); }
-    for (int i = 0; i < C::kA; ++i) {
-      mbar_init(S.bar(C::KFULL + i), 4); mbar_init(S.bar(C::KFREE + i), 1);
-      mbar_init(S.bar(C::VFULL + i), 4); mbar_init(S.bar(C::VFREE + i), 1);
-    }
+    for (int i = 0; i < C::kA; ++i) { mbar_init(S.bar(C::KFULL + i), 4); mbar_init(S.bar(C::VFULL + i), 4); }
     for (int i = 0; i < kScaleBufs; ++i) mbar_init(S.bar(C::SCALE + i), 4);
     for (int i = 0; i < 2; ++i) {
       mbar_init(S.bar(C::SFULL + i), 1); mbar_init(S.bar(C::PFULL + i), 8); mbar_init(S.bar(C::ODONE + i), 1);
@@ -459,7 +468,10 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
   pdl_launch_dependents();
   __syncthreads();
   tc_fence_after();
-  S.tmem = *tmem_slot;
+  // All 512 columns are the CTA's, so they begin at column 0: with the address a constant, the MMA issuer's operands are
+  // constants too (a warp that builds them register by register needs 40 cycles an MMA)
+  S.tmem = 0;
+  if (threadIdx.x == 0 && *tmem_slot != 0) *S.abort_flag = 1;
   const int* prefix = P.tile_prefix;
   const int* slot_info = nullptr;
   if (P.B <= kMaxSmemPrefixSlots) {
@@ -472,34 +484,33 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
   Segment sg;
   const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
 
+  // A decoder writes tile n's buffer when the MMA of tile n - kA has read it.  That is when the scores (the O) of that tile
+  // are announced; before the first tiles the wait is for the phase before the first, which counts as done.
   if (warp < 4) {
     // =========================================================================== K decoders: thread = key of the tile
     regs_dec<C::kRegsDecode>();
-    uint32_t n = 0;
-    const int key = warp * 32 + lane;
-    const uint32_t in_stage = (uint32_t)(key >> 4) * kQTile, t = (uint32_t)key & 15u;
+    uint32_t n = 0, s = 0, full_parity = 0;
+    const uint32_t key = (uint32_t)warp * 32 + (uint32_t)lane;
+    const uint32_t in_k = (key >> 4) * kQTile + (key & 15u) * 16, in_meta = (key >> 4) * kQTile + kQOffMeta + (key & 15u) * 2;
     bool ok = true;
     for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
       for (int j = sg.j0; j < sg.j1; ++j, ++n) {
-        const uint32_t s = n % C::kStages, a = n % C::kA;
-        ok = S.wait(C::FULL + (int)s, n / C::kStages);
-        if (!ok) break;
-        const uint32_t src = S.base + C::kSmRing + s * kStageQ + in_stage;
-        const uint32_t meta = src + kQOffMeta + t * 2;
-        const float sk = __uint_as_float(lds_u16(meta) << 16) * P.scale2, sv = __uint_as_float(lds_u16(meta + 64) << 16);
-        const uint32_t z = lds_u16(meta + 32) * 0x10001u;
-        if (n >= (uint32_t)C::kA) ok = S.wait(C::KFREE + (int)a, n / C::kA - 1);
+        const uint32_t a = n % C::kA, was = n - C::kA;
+        const uint32_t src = S.base + C::kSmRing + s * kStageQ;
+        ok = S.wait(C::FULL + s, full_parity) && S.wait(C::SFULL + (was & 1u), (uint32_t)((int)was >> 1));
         if (!ok) break;
         tc_fence_after();
+        const uint32_t z = lds_u16(src + in_meta + 32) * 0x10001u;
         // QK(n - 2) is done; it was issued after PV(n - 4), which waited until the softmax of tile n - 4 had read its scales
-        asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(S.base + C::kSmScale + ((n % kScaleBufs) * 128 + (uint32_t)key) * 8), "f"(sk), "f"(sv) : "memory");
-        const uint32_t tk = S.tmem + C::kTmK + a * 64 + lane_base;
+        asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(S.base + C::kSmScale + ((n % kScaleBufs) * 128 + key) * 8),
+                     "f"(__uint_as_float(lds_u16(src + in_meta) << 16) * P.scale2), "f"(__uint_as_float(lds_u16(src + in_meta + 64) << 16)) : "memory");
+        const uint32_t tk = C::kTmK + a * 64 + lane_base;
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
+        for (uint32_t h = 0; h < 2; ++h) {
           uint32_t o[32];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const uint4 w = lds128(src + (2 * h + c) * 256 + t * 16);
+            const uint4 w = lds128(src + in_k + h * 512 + c * 256);
             const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int u = 0; u < 4; ++u)
@@ -508,55 +519,56 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
           }
           TMEM_ST32(tk + h * 32, o, 0);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(S.bar(C::EMPTY + (int)s));
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(S.bar(C::KFULL + (int)a));
-          mbar_arrive(S.bar(C::SCALE + (int)(n % kScaleBufs)));
+          mbar_arrive(S.bar(C::KFULL + a));
+          mbar_arrive(S.bar(C::SCALE + n % kScaleBufs));
+          mbar_arrive(S.bar(C::EMPTY + s));
         }
+        if (++s == C::kStages) { s = 0; full_parity ^= 1u; }
       }
     }
   } else if (warp < 8) {
     // =========================================================================== V decoders: thread = dim
     regs_dec<C::kRegsDecode>();
-    uint32_t n = 0;
-    const int dim = (warp & 3) * 32 + lane;
+    uint32_t n = 0, s = 0, full_parity = 0;
+    const uint32_t in_v = kQOffV + (uint32_t)((warp & 3) * 32 + lane) * 8;
     bool ok = true;
     for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
       for (int j = sg.j0; j < sg.j1; ++j, ++n) {
-        const uint32_t s = n % C::kStages, a = n % C::kA;
-        ok = S.wait(C::FULL + (int)s, n / C::kStages);
-        if (ok && n >= (uint32_t)C::kA) ok = S.wait(C::VFREE + (int)a, n / C::kA - 1);
+        const uint32_t a = n % C::kA, was = n - C::kA;
+        const uint32_t src = S.base + C::kSmRing + s * kStageQ;
+        ok = S.wait(C::FULL + s, full_parity) && S.wait(C::ODONE + (was & 1u), (uint32_t)((int)was >> 1));
         if (!ok) break;
         tc_fence_after();
-        const uint32_t src = S.base + C::kSmRing + s * kStageQ;
-        const uint32_t tv = S.tmem + C::kTmV + a * 64 + lane_base;
+        const uint32_t tv = C::kTmV + a * 64 + lane_base;
 #pragma unroll 1
-        for (int h = 0; h < 4; ++h) {
-          uint32_t o[16];
+        for (uint32_t h = 0; h < 2; ++h) {
+          uint32_t o[32];
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const uint32_t pg = src + (uint32_t)(h * 2 + p) * kQTile;
-            const uint2 w = lds64(pg + kQOffV + dim * 8);
+          for (int p = 0; p < 4; ++p) {
+            const uint32_t pg = src + (h * 4 + p) * kQTile;
+            const uint2 w = lds64(pg + in_v);
             const uint4 z0 = lds128(pg + kQOffMeta + 96), z1 = lds128(pg + kQOffMeta + 112);
-            const uint32_t z[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+            const uint32_t zz[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              o[p * 8 + e] = sub_zero(codes_to_bf16(w.x >> (4 * e)), z[e]);
-              o[p * 8 + 4 + e] = sub_zero(codes_to_bf16(w.y >> (4 * e)), z[4 + e]);
+              o[p * 8 + e] = sub_zero(codes_to_bf16(w.x >> (4 * e)), zz[e]);
+              o[p * 8 + 4 + e] = sub_zero(codes_to_bf16(w.y >> (4 * e)), zz[4 + e]);
             }
           }
-          TMEM_ST16(tv + h * 16, o, 0);
+          TMEM_ST32(tv + h * 32, o, 0);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(S.bar(C::EMPTY + (int)s));
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(S.bar(C::VFULL + (int)a));
+        if (lane == 0) {
+          mbar_arrive(S.bar(C::VFULL + a));
+          mbar_arrive(S.bar(C::EMPTY + s));
+        }
+        if (++s == C::kStages) { s = 0; full_parity ^= 1u; }
       }
     }
   } else if (warp < 16) {
@@ -564,138 +576,122 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     regs_inc<C::kRegsSoftmax>();
     uint32_t n = 0;
     bool ok = true;
-    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
-      ok = softmax_segment_q<RMAX>(P, sg, S, (warp - 8) >> 2, n);
-    }
+    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) ok = softmax_segment_q<RMAX>(P, sg, S, (warp - 8) >> 2, n);
   } else {
     regs_dec<C::kRegsRest>();
     if (warp == 16 || warp == 18) {
-      // ========================================================================= page copies, tiles by turns
-      const uint32_t pw = warp == 16 ? 0u : 1u;
-      uint32_t n = 0;
-      bool ok = true;
-      for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
-        const int32_t* pt = P.page_table + (size_t)sg.b * P.max_pages;
-        const int total_pages = (sg.kv_len + ISD_PAGE - 1) / ISD_PAGE;
-        // page ids 32 at a time (4 tiles), one chunk ahead
-        auto load_chunk = [&](int c) -> int {
-          const int pg = sg.j0 * 8 + c * 32 + lane;
-          const int id = pg < total_pages ? pt[pg] : 0;
-          return min(max(id, 0), P.num_pages - 1);
-        };
-        int ids = load_chunk(0), ids_next = load_chunk(1);
-        for (int i = 0; i < sg.j1 - sg.j0; ++i, ++n) {
-          if (i > 0 && (i & 3) == 0) {
-            ids = ids_next;
-            ids_next = load_chunk((i >> 2) + 1);
-          }
-          if ((n & 1u) != pw) continue;
-          const int valid = min(8, total_pages - (sg.j0 + i) * 8);
-          const uint32_t s = n % C::kStages;
-          ok = S.wait(C::EMPTY + (int)s, (n / C::kStages) ^ 1u);
-          if (!ok) break;
-          if (lane == 0) mbar_arrive_expect_tx(S.bar(C::FULL + (int)s), (uint32_t)valid * kQTile);
-          __syncwarp();
-          const int pid = __shfl_sync(0xffffffffu, ids, ((i & 3) << 3) + (lane & 7));
-          if (lane < valid)
-            bulk_g2s(S.base + C::kSmRing + s * kStageQ + lane * kQTile, P.pool + ((size_t)pid * P.Hkv + sg.g) * kQTile, kQTile,
-                     S.bar(C::FULL + (int)s));
-          __syncwarp();
+    // =========================================================================== page copies, tiles by turns
+    const uint32_t pw = warp == 16 ? 0u : 1u;
+    uint32_t n = 0;
+    bool ok = true;
+    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
+      const int32_t* pt = P.page_table + (size_t)sg.b * P.max_pages;
+      const int total_pages = (sg.kv_len + ISD_PAGE - 1) / ISD_PAGE;
+      // page ids 32 at a time (4 tiles), one chunk ahead
+      auto load_chunk = [&](int c) -> int {
+        const int pg = sg.j0 * 8 + c * 32 + lane;
+        const int id = pg < total_pages ? pt[pg] : 0;
+        return min(max(id, 0), P.num_pages - 1);
+      };
+      int ids = load_chunk(0), ids_next = load_chunk(1);
+      for (int i = 0; i < sg.j1 - sg.j0; ++i, ++n) {
+        if (i > 0 && (i & 3) == 0) {
+          ids = ids_next;
+          ids_next = load_chunk((i >> 2) + 1);
         }
-      }
-      if (*S.abort_flag) {  // every issued copy must have landed before the CTA may exit
-        for (uint32_t f = (n > (uint32_t)C::kStages ? n - C::kStages : 0); f < n; ++f)
-          if ((f & 1u) == pw)
-            isd_bounded_wait(P.wait_ns, nullptr, [&]() { return mbar_try_wait(S.bar(C::FULL + (int)(f % C::kStages)), (f / C::kStages) & 1u); });
-      }
-    } else if (warp == 17) {
-      // ========================================================================= MMA issuer
-      uint32_t n = 0;
-      bool ok = true;
-      for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
-        const int cnt = sg.j1 - sg.j0;
-        const uint32_t ncols = (uint32_t)((sg.q_len * P.G + 15) & ~15);
-        const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((ncols >> 3) << 17) | ((128u >> 4) << 24);
-        const uint32_t idesc_pv = idesc_qk | (1u << 16);  // B (= P) is MN-major
-        ok = S.wait(C::QFULL + (int)(seg & 1u), seg >> 1);
+        if ((n & 1u) != pw) continue;
+        const int valid = min(8, total_pages - (sg.j0 + i) * 8);
+        const uint32_t s = n % C::kStages;
+        ok = S.wait(C::EMPTY + s, (n / C::kStages) ^ 1u);
         if (!ok) break;
-        auto qk = [&](uint32_t nn, bool last) -> bool {
-          const uint32_t a = nn % C::kA;
-          if (!S.wait(C::KFULL + (int)a, nn / C::kA)) return false;
-          // S[nn & 1] is free: PV(nn - 2), issued before, waited for P(nn - 2), which was stored after S(nn - 2) was read
-          tc_fence_after();
-          if (elect_one()) {
-            const uint32_t qb = S.base + C::kSmQ + (seg & 1u) * RMAX * 256;
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              tc_mma_ts(S.tmem + C::kTmS + (nn & 1u) * RMAX, S.tmem + C::kTmK + a * 64 + (uint32_t)k * 8u,
-                        smem_desc(qb + (uint32_t)(k >> 2) * (RMAX * 128) + (uint32_t)(k & 3) * 32u, 16, 1024), idesc_qk, k > 0);
-            tc_commit(S.bar(C::KFREE + (int)a));
-            tc_commit(S.bar(C::SFULL + (int)(nn & 1u)));
-            if (last) tc_commit(S.bar(C::QFREE + (int)(seg & 1u)));
-          }
-          __syncwarp();
-          return true;
-        };
-        auto pv = [&](uint32_t nn, bool first) -> bool {
-          const uint32_t a = nn % C::kA;
-          if (!S.wait(C::VFULL + (int)a, nn / C::kA)) return false;
-          if (!S.wait(C::PFULL + (int)(nn & 1u), nn >> 1)) return false;
-          if (first && seg > 0 && !S.wait(C::OFREE, seg - 1u)) return false;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint32_t pb = S.base + C::kSmP + (nn & 1u) * (RMAX / 64) * 16384;
-#pragma unroll
-            for (int k = 0; k < 8; ++k)  // 16 keys = 8 packed columns of V
-              tc_mma_ts(S.tmem + C::kTmO, S.tmem + C::kTmV + a * 64 + (uint32_t)k * 8u, smem_desc(pb + (uint32_t)k * 2048u, 16384, 1024),
-                        idesc_pv, !(first && k == 0));
-            tc_commit(S.bar(C::VFREE + (int)a));
-            tc_commit(S.bar(C::ODONE + (int)(nn & 1u)));
-          }
-          __syncwarp();
-          return true;
-        };
-#pragma unroll 1
-        for (int i = -1; i < cnt && ok; ++i) {
-          if (i + 1 < cnt) ok = qk(n + i + 1, i + 2 == cnt);
-          if (ok && i >= 0) ok = pv(n + i, i == 0);
-        }
-        n += (uint32_t)cnt;
-      }
-    } else {
-      // ========================================================================= segments and their Q, a segment ahead
-      WorkIter<kQuantSegCost> it;
-      it.init(P, cta, prefix, slot_info);
-      bool ok = true;
-      for (uint32_t seg = 0; ok; ++seg) {
-        const bool have = it.next(P, cta, sg);
-        if (!have) sg.b = -1;
-        ok = give_segment<C>(S, seg, sg);
-        if (!have || !ok) break;
-        if (seg >= 2) ok = S.wait(C::QFREE + (int)(seg & 1u), (seg >> 1) - 1u);
-        if (!ok) break;
-        const int rows = sg.q_len * P.G, padded = (rows + 15) & ~15;
-        const uint32_t qb = S.base + C::kSmQ + (seg & 1u) * RMAX * 256;
-        const __nv_bfloat16* src = P.q + ((size_t)sg.b * P.Q * P.Hq + sg.g * P.G) * ISD_HEAD_DIM;
-        const int piece = lane & 15;  // 16 bytes of a row's 256
-        for (int v0 = lane >> 4; v0 < padded; v0 += 8) {  // two rows a step, four steps in flight
-          uint4 x[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int v = v0 + 2 * u;
-            x[u] = make_uint4(0, 0, 0, 0);
-            if (v < rows) x[u] = *reinterpret_cast<const uint4*>(src + ((size_t)(v / P.G) * P.Hq + v % P.G) * ISD_HEAD_DIM + piece * 8);
-          }
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const uint32_t v = (uint32_t)(v0 + 2 * u);
-            sts128(qb + (uint32_t)(piece >> 3) * (RMAX * 128) + v * 128 + ((((uint32_t)piece & 7u) ^ (v & 7u)) << 4), x[u].x, x[u].y, x[u].z, x[u].w);
-          }
-        }
-        fence_async_smem();
+        if (lane == 0) mbar_arrive_expect_tx(S.bar(C::FULL + s), (uint32_t)valid * kQTile);
         __syncwarp();
-        if (lane == 0) mbar_arrive(S.bar(C::QFULL + (int)(seg & 1u)));
+        const int pid = __shfl_sync(0xffffffffu, ids, ((i & 3) << 3) + (lane & 7));
+        if (lane < valid)
+          ring_bulk_g2s(S.base + C::kSmRing + s * kStageQ + lane * kQTile, P.pool + ((size_t)pid * P.Hkv + sg.g) * kQTile, kQTile,
+                        S.bar(C::FULL + s));
+        __syncwarp();
       }
+    }
+    if (*S.abort_flag) {  // every issued copy must have landed before the CTA may exit
+      for (uint32_t f = (n > (uint32_t)C::kStages ? n - C::kStages : 0); f < n; ++f)
+        if ((f & 1u) == pw)
+          isd_bounded_wait(P.wait_ns, nullptr, [&]() { return mbar_try_wait(S.bar(C::FULL + f % C::kStages), (f / C::kStages) & 1u); });
+    }
+    } else if (warp == 17) {
+    // =========================================================================== MMA issuer
+    uint32_t n = 0;
+    bool ok = true;
+    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
+      const int cnt = sg.j1 - sg.j0;
+      const uint32_t ncols = (uint32_t)((sg.q_len * P.G + 15) & ~15);
+      const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((ncols >> 3) << 17) | ((128u >> 4) << 24);
+      const uint32_t idesc_pv = idesc_qk | (1u << 16);  // B (= P) is MN-major
+      const uint64_t q_desc = smem_desc(S.base + C::kSmQ + (seg & 1u) * RMAX * 256, 16, 1024);
+      ok = S.wait(C::QFULL + (seg & 1u), seg >> 1);
+      if (!ok) break;
+#pragma unroll 1
+      for (int i = -1; i < cnt; ++i) {
+        if (i + 1 < cnt) {  // QK of the next tile
+          const uint32_t nn = n + (uint32_t)(i + 1);
+          ok = S.wait(C::KFULL + nn % C::kA, nn / C::kA);
+          if (!ok) break;
+          // S is free: PV(nn - 2), issued before, waited for P(nn - 2), which was stored after S(nn - 2) was read
+          tc_fence_after();
+          if (elect_one()) {
+            if (nn & 1u) issue_qk<RMAX, 1>(S, q_desc, idesc_qk); else issue_qk<RMAX, 0>(S, q_desc, idesc_qk);
+            if (i + 2 == cnt) tc_commit(S.bar(C::QFREE + (seg & 1u)));
+          }
+          __syncwarp();
+        }
+        if (i >= 0) {  // PV of this tile
+          const uint32_t nn = n + (uint32_t)i;
+          ok = S.wait(C::VFULL + nn % C::kA, nn / C::kA) && S.wait(C::PFULL + (nn & 1u), nn >> 1);
+          if (ok && i == 0 && seg > 0) ok = S.wait(C::OFREE, seg - 1u);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            if (nn & 1u) issue_pv<RMAX, 1>(S, idesc_pv, i > 0); else issue_pv<RMAX, 0>(S, idesc_pv, i > 0);
+          }
+          __syncwarp();
+        }
+      }
+      n += (uint32_t)cnt;
+    }
+    } else {
+    // =========================================================================== segments and their Q, a segment ahead
+    WorkIter<kQuantSegCost> it;
+    it.init(P, cta, prefix, slot_info);
+    bool ok = true;
+    for (uint32_t seg = 0; ok; ++seg) {
+      const bool have = it.next(P, cta, sg);
+      if (!have) sg.b = -1;
+      ok = give_segment<C>(S, seg, sg);
+      if (!have || !ok) break;
+      if (seg >= 2) ok = S.wait(C::QFREE + (seg & 1u), (seg >> 1) - 1u);
+      if (!ok) break;
+      const int rows = sg.q_len * P.G, padded = (rows + 15) & ~15;
+      const uint32_t qb = S.base + C::kSmQ + (seg & 1u) * RMAX * 256;
+      const __nv_bfloat16* src = P.q + ((size_t)sg.b * P.Q * P.Hq + sg.g * P.G) * ISD_HEAD_DIM;
+      const int piece = lane & 15;  // 16 bytes of a row's 256
+      for (int v0 = lane >> 4; v0 < padded; v0 += 8) {  // two rows a step, four steps in flight
+        uint4 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int v = v0 + 2 * u;
+          x[u] = make_uint4(0, 0, 0, 0);
+          if (v < rows) x[u] = *reinterpret_cast<const uint4*>(src + ((size_t)(v / P.G) * P.Hq + v % P.G) * ISD_HEAD_DIM + piece * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t v = (uint32_t)(v0 + 2 * u);
+          sts128(qb + (uint32_t)(piece >> 3) * (RMAX * 128) + v * 128 + ((((uint32_t)piece & 7u) ^ (v & 7u)) << 4), x[u].x, x[u].y, x[u].z, x[u].w);
+        }
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(S.bar(C::QFULL + (seg & 1u)));
+    }
     }
   }
 
@@ -710,7 +706,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
 }
 
 template <int RMAX>
-cudaError_t launch_main(const isd_ctx* ctx, const QuantParams& P, cudaStream_t stream) {
+cudaError_t launch_main(const QuantParams& P, cudaStream_t stream) {
   return isd_launch_pdl(attn_quant_kernel<RMAX>, dim3(P.num_ctas), dim3(kQuantThreads), Cfg<RMAX>::kSmemBytes, stream, P);
 }
 
@@ -743,7 +739,7 @@ int isd_launch_attn_quant(isd_ctx* ctx, const isd_batch_state* st, const void* q
   cudaError_t e = cudaSuccess;
   if (c.batch > kMaxSmemPrefixSlots) e = isd_launch_pdl(attn_plan_kernel<kQuantSegCost>, dim3(1), dim3(1024), 0, stream, P);
   if (ctx->ev_attn0) cudaEventRecord(ctx->ev_attn0, stream);
-  if (e == cudaSuccess) e = ctx->G * ctx->Q <= 64 ? launch_main<64>(ctx, P, stream) : launch_main<128>(ctx, P, stream);
+  if (e == cudaSuccess) e = ctx->G * ctx->Q <= 64 ? launch_main<64>(P, stream) : launch_main<128>(P, stream);
   if (ctx->ev_attn1) cudaEventRecord(ctx->ev_attn1, stream);
   if (e == cudaSuccess) e = isd_launch_pdl(attn_combine_kernel<kQuantSegCost, false>, dim3(P.num_ctas), dim3(kCombineThreads), 0, stream, P);
   ctx->launches += 2 + (c.batch > kMaxSmemPrefixSlots ? 1 : 0);
