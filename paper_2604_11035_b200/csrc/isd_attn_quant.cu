@@ -72,8 +72,12 @@ struct Cfg {
   static constexpr uint32_t kTmK = 0, kTmV = kTmK + kA * 64, kTmS = kTmV + kA * 64, kTmO = kTmS + 2 * RMAX;
   static_assert(kTmO + RMAX <= 512 && kSmemBytes <= 232448, "tensor memory / shared memory");
   enum {
-    FULL = 0, EMPTY = FULL + kStages, KFULL = EMPTY + kStages, VFULL = KFULL + kA, SCALE = VFULL + kA, SFULL = SCALE + kScaleBufs, PFULL = SFULL + 2,
-    ODONE = PFULL + 2, QFULL = ODONE + 2, QFREE = QFULL + 2, OFREE = QFREE + 2, SEGFULL, SEGFREE = SEGFULL + 4, COUNT = SEGFREE + 4
+    FULL = 0, EMPTY = FULL + kStages,  // ring stages
+    KFULL = EMPTY + kStages,           // decoded K in tensor memory
+    SFULL = KFULL + kA,                // scores in tensor memory (the MMAs' commit) and the tile's scales in shared memory (decoders)
+    PVFULL = SFULL + 2,                // P in shared memory (softmax) and decoded V in tensor memory (decoders)
+    ODONE = PVFULL + 2,                // PV done
+    QFULL = ODONE + 2, QFREE = QFULL + 2, OFREE = QFREE + 2, SEGFULL, SEGFREE = SEGFULL + 4, COUNT = SEGFREE + 4
   };
   static_assert(COUNT * 8 + 32 <= 512, "barrier block");
   // Registers a thread: 640 threads are launched with 96 each and share them out anew.
@@ -138,13 +142,24 @@ __device__ __forceinline__ bool mbar_try_wait_long(uint32_t bar, uint32_t parity
   return ok != 0;
 }
 
+// one look at a phase; a try_wait that finds its phase complete still costs 150 cycles with a suspension limit
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+
 struct Shared {  // what every role needs
   uint8_t* smem;
   uint32_t base, bar0, tmem;
   volatile int* abort_flag;
   __device__ __forceinline__ uint32_t bar(uint32_t i) const { return bar0 + 8u * i; }
   __device__ __forceinline__ bool wait(uint32_t i, uint32_t parity) const {
-    if (mbar_try_wait_long(bar(i), parity & 1u)) return true;
+    if (mbar_test(bar(i), parity & 1u)) return true;
     unsigned long long t0 = 0;  // (at most one more suspension after another thread has given up)
     while (!mbar_try_wait_long(bar(i), parity & 1u)) {
       const unsigned long long now = isd_now_ns();
@@ -161,14 +176,14 @@ struct Shared {  // what every role needs
 
 // The CTA's segments are worked out by one warp and handed to the other roles through a ring in shared memory: the
 // enumeration (64-bit divisions) would otherwise sit in every role's code, and the roles share one instruction cache.
-template <class C>
+template <class C, bool ONE_THREAD = false>
 __device__ __forceinline__ bool take_segment(const Shared& S, uint32_t k, Segment& sg) {
   const uint32_t i = k % kSegRing;
   if (!S.wait(C::SEGFULL + i, k / kSegRing)) return false;
   const int4* src = reinterpret_cast<const int4*>(S.smem + C::kSmSeg) + 2 * i;
   const int4 a = src[0], b = src[1];
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(S.bar(C::SEGFREE + i));
+  if (!ONE_THREAD) __syncwarp();
+  if (ONE_THREAD || (threadIdx.x & 31) == 0) mbar_arrive(S.bar(C::SEGFREE + i));
   sg.b = a.x; sg.g = a.y; sg.j0 = a.z; sg.j1 = a.w;
   sg.ctx = b.x; sg.q_len = b.y; sg.part_slot = b.z;
   sg.kv_len = sg.ctx + sg.q_len;
@@ -212,10 +227,9 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
   const uint32_t sw = ((uint32_t)tl & 7u) << 4, p_row = S.base + C::kSmP + (uint32_t)tl * 128;
   for (int i = 0; i < cnt; ++i) {
     const uint32_t nn = n + (uint32_t)i, buf = nn & 1u;
-    if (!S.wait(C::SCALE + nn % kScaleBufs, nn / kScaleBufs)) return false;
+    if (!S.wait(C::SFULL + buf, nn >> 1)) return false;
     const uint2 scl = lds64(S.base + C::kSmScale + ((nn % kScaleBufs) * 128 + (uint32_t)tl) * 8);
     float sk = __uint_as_float(scl.x), sv = __uint_as_float(scl.y);
-    if (!S.wait(C::SFULL + buf, nn >> 1)) return false;
     if (mine > 0) {
       tc_fence_after();
       const uint32_t ts = S.tmem + C::kTmS + buf * RMAX + (uint32_t)c0 * 16 + lane_base;
@@ -338,7 +352,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
       tc_fence_before();
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(S.bar(C::PFULL + buf));
+    if (lane == 0) mbar_arrive(S.bar(C::PVFULL + buf));
   }
   // ---- row sums over the lanes: exchange halves until lane k of a warp holds the sum of row k of a 32-row group
 #pragma unroll
@@ -442,10 +456,9 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
   // ---- set-up that touches nothing an earlier kernel wrote
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) { mbar_init(S.bar(C::FULL + i), 1); mbar_init(S.bar(C::EMPTY + i), 8); }
-    for (int i = 0; i < C::kA; ++i) { mbar_init(S.bar(C::KFULL + i), 4); mbar_init(S.bar(C::VFULL + i), 4); }
-    for (int i = 0; i < kScaleBufs; ++i) mbar_init(S.bar(C::SCALE + i), 4);
+    for (int i = 0; i < C::kA; ++i) mbar_init(S.bar(C::KFULL + i), 4);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(S.bar(C::SFULL + i), 1); mbar_init(S.bar(C::PFULL + i), 8); mbar_init(S.bar(C::ODONE + i), 1);
+      mbar_init(S.bar(C::SFULL + i), 1 + 4); mbar_init(S.bar(C::PVFULL + i), 8 + 4); mbar_init(S.bar(C::ODONE + i), 1);
       mbar_init(S.bar(C::QFULL + i), 1); mbar_init(S.bar(C::QFREE + i), 1);
     }
     mbar_init(S.bar(C::OFREE), 8);
@@ -501,7 +514,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
         if (!ok) break;
         tc_fence_after();
         const uint32_t z = lds_u16(src + in_meta + 32) * 0x10001u;
-        // QK(n - 2) is done; it was issued after PV(n - 4), which waited until the softmax of tile n - 4 had read its scales
+        // QK(n - 2) is done; it was issued after PV(n - 4) was, which waited until the softmax of tile n - 4 had read its scales
         asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(S.base + C::kSmScale + ((n % kScaleBufs) * 128 + key) * 8),
                      "f"(__uint_as_float(lds_u16(src + in_meta) << 16) * P.scale2), "f"(__uint_as_float(lds_u16(src + in_meta + 64) << 16)) : "memory");
         const uint32_t tk = C::kTmK + a * 64 + lane_base;
@@ -523,8 +536,8 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
+          mbar_arrive(S.bar(C::SFULL + (n & 1u)));
           mbar_arrive(S.bar(C::KFULL + a));
-          mbar_arrive(S.bar(C::SCALE + n % kScaleBufs));
           mbar_arrive(S.bar(C::EMPTY + s));
         }
         if (++s == C::kStages) { s = 0; full_parity ^= 1u; }
@@ -565,7 +578,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(S.bar(C::VFULL + a));
+          mbar_arrive(S.bar(C::PVFULL + (n & 1u)));
           mbar_arrive(S.bar(C::EMPTY + s));
         }
         if (++s == C::kStages) { s = 0; full_parity ^= 1u; }
@@ -579,9 +592,8 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) ok = softmax_segment_q<RMAX>(P, sg, S, (warp - 8) >> 2, n);
   } else {
     regs_dec<C::kRegsRest>();
-    if (warp == 16 || warp == 18) {
-    // =========================================================================== page copies, tiles by turns
-    const uint32_t pw = warp == 16 ? 0u : 1u;
+    if (warp == 16) {
+    // =========================================================================== page copies
     uint32_t n = 0;
     bool ok = true;
     for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
@@ -599,7 +611,6 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
           ids = ids_next;
           ids_next = load_chunk((i >> 2) + 1);
         }
-        if ((n & 1u) != pw) continue;
         const int valid = min(8, total_pages - (sg.j0 + i) * 8);
         const uint32_t s = n % C::kStages;
         ok = S.wait(C::EMPTY + s, (n / C::kStages) ^ 1u);
@@ -615,49 +626,49 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     }
     if (*S.abort_flag) {  // every issued copy must have landed before the CTA may exit
       for (uint32_t f = (n > (uint32_t)C::kStages ? n - C::kStages : 0); f < n; ++f)
-        if ((f & 1u) == pw)
-          isd_bounded_wait(P.wait_ns, nullptr, [&]() { return mbar_try_wait(S.bar(C::FULL + f % C::kStages), (f / C::kStages) & 1u); });
+        isd_bounded_wait(P.wait_ns, nullptr, [&]() { return mbar_try_wait(S.bar(C::FULL + f % C::kStages), (f / C::kStages) & 1u); });
     }
     } else if (warp == 17) {
-    // =========================================================================== MMA issuer
-    uint32_t n = 0;
-    bool ok = true;
-    for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) {
-      const int cnt = sg.j1 - sg.j0;
-      const uint32_t ncols = (uint32_t)((sg.q_len * P.G + 15) & ~15);
-      const uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((ncols >> 3) << 17) | ((128u >> 4) << 24);
-      const uint32_t idesc_pv = idesc_qk | (1u << 16);  // B (= P) is MN-major
-      const uint64_t q_desc = smem_desc(S.base + C::kSmQ + (seg & 1u) * RMAX * 256, 16, 1024);
-      ok = S.wait(C::QFULL + (seg & 1u), seg >> 1);
-      if (!ok) break;
+    // =========================================================================== QK issuer: one thread from here on
+    if (elect_one()) {
+      uint32_t n = 0;
+      bool ok = true;
+      for (uint32_t seg = 0; ok && take_segment<C, true>(S, seg, sg); ++seg) {
+        const uint32_t ncols = (uint32_t)((sg.q_len * P.G + 15) & ~15);
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((ncols >> 3) << 17) | ((128u >> 4) << 24);
+        const uint64_t q_desc = smem_desc(S.base + C::kSmQ + (seg & 1u) * RMAX * 256, 16, 1024);
+        ok = S.wait(C::QFULL + (seg & 1u), seg >> 1);
 #pragma unroll 1
-      for (int i = -1; i < cnt; ++i) {
-        if (i + 1 < cnt) {  // QK of the next tile
-          const uint32_t nn = n + (uint32_t)(i + 1);
-          ok = S.wait(C::KFULL + nn % C::kA, nn / C::kA);
+        for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+          // PV(n - 2) is done: the softmax has read the scores that were in this buffer, and P's buffer is free when it sees the new ones
+          ok = S.wait(C::ODONE + (n & 1u), (uint32_t)(((int)n - 2) >> 1)) && S.wait(C::KFULL + n % C::kA, n / C::kA);
           if (!ok) break;
-          // S is free: PV(nn - 2), issued before, waited for P(nn - 2), which was stored after S(nn - 2) was read
           tc_fence_after();
-          if (elect_one()) {
-            if (nn & 1u) issue_qk<RMAX, 1>(S, q_desc, idesc_qk); else issue_qk<RMAX, 0>(S, q_desc, idesc_qk);
-            if (i + 2 == cnt) tc_commit(S.bar(C::QFREE + (seg & 1u)));
-          }
-          __syncwarp();
+          if (n & 1u) issue_qk<RMAX, 1>(S, q_desc, idesc); else issue_qk<RMAX, 0>(S, q_desc, idesc);
         }
-        if (i >= 0) {  // PV of this tile
-          const uint32_t nn = n + (uint32_t)i;
-          ok = S.wait(C::VFULL + nn % C::kA, nn / C::kA) && S.wait(C::PFULL + (nn & 1u), nn >> 1);
-          if (ok && i == 0 && seg > 0) ok = S.wait(C::OFREE, seg - 1u);
+        if (ok) tc_commit(S.bar(C::QFREE + (seg & 1u)));
+      }
+    }
+    __syncwarp();
+    } else if (warp == 18) {
+    // =========================================================================== PV issuer: one thread
+    if (elect_one()) {
+      uint32_t n = 0;
+      bool ok = true;
+      for (uint32_t seg = 0; ok && take_segment<C, true>(S, seg, sg); ++seg) {
+        const uint32_t ncols = (uint32_t)((sg.q_len * P.G + 15) & ~15);
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((ncols >> 3) << 17) | ((128u >> 4) << 24);  // B (= P) is MN-major
+        if (seg > 0) ok = S.wait(C::OFREE, seg - 1u);
+#pragma unroll 1
+        for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+          ok = S.wait(C::PVFULL + (n & 1u), n >> 1);
           if (!ok) break;
           tc_fence_after();
-          if (elect_one()) {
-            if (nn & 1u) issue_pv<RMAX, 1>(S, idesc_pv, i > 0); else issue_pv<RMAX, 0>(S, idesc_pv, i > 0);
-          }
-          __syncwarp();
+          if (n & 1u) issue_pv<RMAX, 1>(S, idesc, j > sg.j0); else issue_pv<RMAX, 0>(S, idesc, j > sg.j0);
         }
       }
-      n += (uint32_t)cnt;
     }
+    __syncwarp();
     } else {
     // =========================================================================== segments and their Q, a segment ahead
     WorkIter<kQuantSegCost> it;
