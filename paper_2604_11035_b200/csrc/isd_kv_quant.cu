@@ -1,7 +1,7 @@
 // The 4-bit KV cache's traffic: the block append of isd_attn_quant, isd_kv_write_quant and isd_kv_read_quant
 // (Sec. 3.3 (2): KV rows enter the paged cache by one batched scatter).
 //
-// All three work on runs of consecutive tokens inside a page, one warp per (run, kv head): a V word holds eight
+// The latter two work on runs of consecutive tokens inside a page, one warp per (run, kv head): a V word holds eight
 // tokens of a dim, so a run's words are built in registers and stored whole.
 #include "isd_quant.cuh"
 
@@ -20,17 +20,30 @@ struct AppendParams {
   uint8_t* pool;
 };
 
-constexpr int kAppendWarps = 3;  // a block of up to 31 rows lies in at most three pages
+constexpr int kAppendThreads = 256;
+constexpr int kAppendRounds = 4;  // of 16 half-warps: 2 * 31 rows at most
 
-// One CTA per (slot, kv head): validate the slot's page-table prefix, then a warp per page of the block.
-__global__ void __launch_bounds__(kAppendWarps * 32) kv_append_quant_kernel(const AppendParams P) {
+// One CTA per (slot, kv head): validate the slot's page-table prefix, quantise the block's rows (a half-warp per row of K or
+// V), then put V's words together.  The kernel is a chain of latencies (state, pages, rows) in front of the attention's first
+// copy, so the rows are fetched before the state says how many there are, and all rows are encoded side by side: with a
+// warp per page, which encodes its rows one after the other, it took three times as long.
+__global__ void __launch_bounds__(kAppendThreads) kv_append_quant_kernel(const AppendParams P) {
+  __shared__ uint2 codes[ISD_MAX_Q + 1][16];  // V codes, a byte each: [row][eight dims]
   const int b = blockIdx.x, g = blockIdx.y;
+  const int hw = threadIdx.x >> 4, hl = threadIdx.x & 15;
   pdl_wait();
   pdl_launch_dependents();
-  if (!P.active[b]) return;
-  const int nv = P.n_ver[b];
-  if (nv < 0 || nv > P.N - 1) return;
-  const int ql = nv + P.N, ctx = P.ctx_len[b];
+  const size_t stride = (size_t)P.Hkv * ISD_HEAD_DIM;
+  uint4 x[kAppendRounds];
+#pragma unroll
+  for (int i = 0; i < kAppendRounds; ++i) {
+    const int row = (i * 16 + hw) >> 1;
+    const __nv_bfloat16* src = (hw & 1) ? P.v_new : P.k_new;
+    x[i] = row < P.Q ? *reinterpret_cast<const uint4*>(src + ((size_t)b * P.Q + row) * stride + (size_t)g * ISD_HEAD_DIM + hl * 8) : make_uint4(0, 0, 0, 0);
+  }
+  const int nv = P.n_ver[b], ctx = P.ctx_len[b];
+  if (!P.active[b] || nv < 0 || nv > P.N - 1) return;
+  const int ql = nv + P.N;
   // (a length near 2^31 must not wrap: compare before adding)
   if (ctx < 0 || ctx > (long long)P.max_pages * ISD_PAGE - ql) {
     if (threadIdx.x == 0 && g == 0) {
@@ -39,10 +52,11 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_quant_kernel(cons
     }
     return;
   }
-  const int pages = (ctx + ql + ISD_PAGE - 1) / ISD_PAGE;
+  const int pages = (ctx + ql + ISD_PAGE - 1) / ISD_PAGE, page0 = ctx / ISD_PAGE, off0 = ctx % ISD_PAGE;
   const int32_t* pt = P.page_table + (size_t)b * P.max_pages;
   int bad = 0;
-  for (int pg = threadIdx.x; pg < pages; pg += blockDim.x) {
+#pragma unroll 4
+  for (int pg = threadIdx.x; pg < pages; pg += kAppendThreads) {
     const int id = pt[pg];
     bad |= id < 0 || id >= P.num_pages;
   }
@@ -53,23 +67,53 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_quant_kernel(cons
     }
     return;
   }
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int pg = ctx / ISD_PAGE + warp;
-  if (pg >= pages) return;
-  const int off = warp == 0 ? ctx % ISD_PAGE : 0;
-  const int row0 = warp == 0 ? 0 : warp * ISD_PAGE - ctx % ISD_PAGE;
-  const int cnt = min(ISD_PAGE - off, ql - row0);
-  uint8_t* tile = P.pool + ((size_t)pt[pg] * P.Hkv + g) * kQTile;
-  const size_t stride = (size_t)P.Hkv * ISD_HEAD_DIM;
-  const size_t src = ((size_t)b * P.Q + row0) * stride + (size_t)g * ISD_HEAD_DIM;
-  quant_store_run<false>(P.k_new + src, stride, P.v_new + src, stride, tile, off, cnt);
+  auto tile_of = [&](int pg) { return P.pool + ((size_t)pt[pg] * P.Hkv + g) * kQTile; };
+#pragma unroll
+  for (int i = 0; i < kAppendRounds; ++i) {
+    if (i * 8 >= ql) break;
+    const int row = (i * 16 + hw) >> 1;
+    const QuantParam p = quant_half_warp(x[i]);
+    float f[8];
+    unpack8(x[i], f);
+    uint32_t c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = quant_code(f[e], p);
+    if (row < ql) {
+      const int t = (off0 + row) % ISD_PAGE;
+      uint8_t* tile = tile_of((ctx + row) / ISD_PAGE);
+      if (hw & 1) {
+        codes[row][hl] = make_uint2(c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24), c[4] | (c[5] << 8) | (c[6] << 16) | (c[7] << 24));
+      } else {
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w |= c[e] << (4 * (e >> 1) + 16 * (e & 1));
+        *reinterpret_cast<uint32_t*>(tile + (hl >> 2) * 256 + t * 16 + (hl & 3) * 4) = w;
+      }
+      if (hl < 2) reinterpret_cast<uint16_t*>(tile + kQOffMeta)[((hw & 1) * 2 + hl) * 16 + t] = hl == 0 ? p.s_bits : p.z_bits;
+    }
+  }
+  __syncthreads();
+  // V words: (page of the block, dim, half of the page)
+  const uint8_t* bytes = reinterpret_cast<const uint8_t*>(codes);
+  for (int i = threadIdx.x; i < (pages - page0) * 256; i += kAppendThreads) {
+    const int pg = i >> 8, half = (i >> 7) & 1, dim = i & 127;
+    const int row0 = pg * ISD_PAGE + half * 8 - off0;  // row of the word's first token
+    if (row0 >= ql || row0 + 8 <= 0) continue;
+    uint32_t w = 0, mask = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int row = row0 + e, sh = 4 * (e >> 1) + 16 * (e & 1);
+      if (row >= 0 && row < ql) w |= (uint32_t)bytes[row * ISD_HEAD_DIM + dim] << sh;
+      if (row < 0) mask |= 0xFu << sh;
+    }
+    uint32_t* dst = reinterpret_cast<uint32_t*>(tile_of(page0 + pg) + kQOffV) + dim * 2 + half;
+    *dst = mask ? (*dst & mask) | w : w;  // committed tokens of the word stay
+  }
   // Tokens behind the block are emptied: their probability is zero, but the tensor cores multiply it by code minus zero,
   // which needs a finite zero.
-  if (pg == pages - 1) {
-    uint16_t* meta = reinterpret_cast<uint16_t*>(tile + kQOffMeta);
-    for (int i = lane; i < 64; i += 32)
-      if ((i & 15) >= off + cnt) meta[i] = (i & 16) ? kQZeroOne : (uint16_t)0;
-  }
+  const int end = off0 + ql - (pages - 1 - page0) * ISD_PAGE;  // tokens of the last page up to the block's end
+  if (threadIdx.x < 64 && (int)(threadIdx.x & 15) >= end)
+    reinterpret_cast<uint16_t*>(tile_of(pages - 1) + kQOffMeta)[threadIdx.x] = (threadIdx.x & 16) ? kQZeroOne : (uint16_t)0;
 }
 
 struct RowsParams {
@@ -122,7 +166,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32) kv_write_quant_kernel(const R
   pdl_wait();
   pdl_launch_dependents();
   for_runs(P, [&](int64_t t, int off, int cnt, uint8_t* tile, int g) {
-    quant_store_run<true>(P.k + (size_t)t * P.k_stride + g * ISD_HEAD_DIM, P.k_stride,
+    quant_store_run(P.k + (size_t)t * P.k_stride + g * ISD_HEAD_DIM, P.k_stride,
                           P.v + (size_t)t * P.v_stride + g * ISD_HEAD_DIM, P.v_stride, tile, off, cnt);
   });
 }
@@ -201,7 +245,7 @@ int isd_launch_kv_append_quant(isd_ctx* ctx, const isd_batch_state* st, const vo
   P.ctx_len = st->ctx_len; P.n_ver = st->n_ver; P.active = st->active; P.page_table = st->page_table;
   P.slot_status = st->slot_status; P.global_status = ctx->global_status;
   P.k_new = (const __nv_bfloat16*)k_new; P.v_new = (const __nv_bfloat16*)v_new; P.pool = (uint8_t*)kv_pool;
-  const cudaError_t e = isd_launch_pdl(kv_append_quant_kernel, dim3(c.batch, c.n_kv_heads), dim3(kAppendWarps * 32), 0, stream, P);
+  const cudaError_t e = isd_launch_pdl(kv_append_quant_kernel, dim3(c.batch, c.n_kv_heads), dim3(kAppendThreads), 0, stream, P);
   ctx->launches++;
   return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }

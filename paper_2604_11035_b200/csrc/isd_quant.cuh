@@ -1,5 +1,5 @@
 // The 4-bit KV cache: tile layout, codec and the warp routine that stores a run of tokens (layout and codec are
-// stated in include/isd.h).  Shared by the block append of isd_attn_quant and by isd_kv_write_quant.
+// stated in include/isd.h).
 #pragma once
 #include "isd_internal.cuh"
 
@@ -103,9 +103,8 @@ __device__ __forceinline__ uint32_t token_mask(int off, int cnt, int word) {
 
 // One warp stores tokens off .. off + cnt - 1 of a page (source rows 0 .. cnt - 1 of k and v, already offset to the kv
 // head) into the page's tile.  Lane = (parity of the token) * 16 + chunk of eight dims, so that a row is read in 16-byte
-// pieces and the even tokens of a V word meet the odd ones in one exchange.  ATOMIC: other warps may be writing other
-// tokens of the same tile (V words hold eight tokens); their nibbles are disjoint, so clearing and setting bits commutes.
-template <bool ATOMIC>
+// pieces and the even tokens of a V word meet the odd ones in one exchange.  Other warps may be writing other tokens of the
+// same tile (V words hold eight tokens); their nibbles are disjoint, so clearing and setting bits commutes.
 __device__ __forceinline__ void quant_store_run(const __nv_bfloat16* k, size_t k_stride, const __nv_bfloat16* v,
                                                 size_t v_stride, uint8_t* tile, int off, int cnt) {
   const int lane = threadIdx.x & 31, hl = lane & 15, par = lane >> 4;
@@ -160,15 +159,11 @@ __device__ __forceinline__ void quant_store_run(const __nv_bfloat16* k, size_t k
     for (int e = 0; e < 8; ++e) {
       const uint32_t m = (e & 1) ? m1 : m0;
       if (m == 0) continue;
-      if (ATOMIC) {
-        if (m != 0xFFFFFFFFu) {
-          atomicAnd(dst + e, ~m);
-          atomicOr(dst + e, o[e] & m);
-        } else {
-          dst[e] = o[e];
-        }
+      if (m != 0xFFFFFFFFu) {
+        atomicAnd(dst + e, ~m);
+        atomicOr(dst + e, o[e] & m);
       } else {
-        dst[e] = (dst[e] & ~m) | (o[e] & m);
+        dst[e] = o[e];
       }
     }
   }
