@@ -1,119 +1,444 @@
-// isd_logprobs: log probability of given tokens, entropy and top alternatives of their rows' laws.
-// One CTA per entry: a pass for the maximum and the sums, then a pass per alternative.
+// isd_logprobs: log probability of given tokens, entropy and top alternatives of their rows' laws, in one pass over a row.
+//
+// With y = x * invT * log2(e) and any reference r, the pass sums s = sum 2^(y - r) and w = sum 2^(y - r) (y - r); then
+//     log p(x) = (x - max) invT - ln s',    H = ln s' - ln 2 * w' / s'       (s', w': moved to r = the row's maximum).
+// The reference is a warp's: it is raised only when a logit passes it by more than 2^8, which after the first few vectors
+// hardly happens, so the loop has no other reduction in it.
+//
+// Top alternatives without a test per element: the pass keeps each thread's maximum (which the reference needs anyway).  The
+// top_n-th largest of the 256 maxima is a lower bound of the row's top_n-th value, and only threads whose maximum reaches it
+// can hold an alternative: their elements (top_n of 256 columns of the row, still in L2) are looked at again, by warps that
+// keep a sorted list, one key per lane.  Ties go to the lower index through the key (order-preserving code of the value,
+// complement of the index).
+//
+// Bound: HBM (a row is read once; 12 logits a cycle and SM at the measured copy rate), 5 instructions and one exponential a
+// logit.  Few rows are cut into pieces, whose partial results the last piece to finish merges.
+#include <string.h>
+
 #include "isd_internal.cuh"
 
 namespace {
+
+constexpr int kLpThreads = 256;
+constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kLpPerSm = 4;        // resident CTAs
+constexpr int kLpMaxPieces = 32;
+constexpr int kLpMaxParts = 4096;  // pieces of all rows of a call that cuts them
+constexpr int kLpUnroll = 4;       // 16-byte vectors a thread has in flight, twice
+
+struct LpPart {
+  float m, s, w;  // maximum, sums
+  float pad;
+  unsigned long long key[ISD_MAX_TOP_LOGPROBS];  // the piece's alternatives, best first
+};
 
 struct LogprobsParams {
   const void* logits;
   int64_t logits_rows;
   const int32_t* rows;
   const int32_t* tokens;
-  int n, V, top_n, dtype;
-  float inv_t;
+  int V, top_n, pieces;
+  float inv_t, scale2, floor;  // scale2 = invT * log2(e); floor: logits below it (about -1e36 / scale2) count as equal to it, so that no product with a zero probability is NaN
   float* logprob;
   float* entropy;
   int32_t* top_id;
   float* top_logprob;
   uint32_t* global_status;
+  LpPart* part;
+  int* ticket;
 };
 
-constexpr int kLpThreads = 256;
+typedef unsigned long long u64;
 
-template <class T, class Op>
-__device__ T block_reduce(T v, T* sm, Op op) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, off));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = sm[0];
-#pragma unroll
-  for (int w = 1; w < kLpThreads / 32; ++w) v = op(v, sm[w]);
-  return v;
-}
-
-// order-preserving code of a float (-0 and 0 alike), and the sort key of (value, index): larger value first, then lower index
+// order-preserving code of a float (-0 and 0 alike), and back
 __device__ __forceinline__ uint32_t order_code(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+__device__ __forceinline__ float order_value(uint32_t c) { return __uint_as_float((c & 0x80000000u) ? (c & 0x7FFFFFFFu) : ~c); }
+__device__ __forceinline__ u64 lp_key(float x, int idx) { return ((u64)order_code(x) << 32) | (0xFFFFFFFFu - (uint32_t)idx); }
 
-__global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const LogprobsParams P) {
-  __shared__ float smf[8];
-  __shared__ unsigned long long smk[8];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int i = blockIdx.x, tok = P.tokens[i];
-  const int64_t row = P.rows ? P.rows[i] : i;
-  uint32_t why = 0;
-  if (tok >= P.V || (tok >= 0 && (row < 0 || row >= P.logits_rows))) why = ISD_ST_BAD_TOKEN_ID;
-  bool skip = tok < 0 || why;
-  float m = -INFINITY, s = 0.f, w = 0.f;
-  const size_t base = skip ? 0 : (size_t)row * P.V;
-  if (!skip) {
-    float bad = 0.f;
-    for (int v = threadIdx.x; v < P.V; v += kLpThreads) {
-      const float x = load_logit(P.logits, P.dtype, base + v);
-      if (!(x < INFINITY)) bad = 1.f;
-      m = fmaxf(m, x);
-    }
-    auto fmx = [](float a, float b) { return fmaxf(a, b); };
-    bad = block_reduce(bad, smf, fmx);
-    m = block_reduce(m, smf, fmx);
-    if (bad > 0.f || m == -INFINITY) {
-      why = ISD_ST_NONFINITE_LOGIT;
-      skip = true;
+__device__ __forceinline__ float lp_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lp_warp_max(float x) {
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t hmax2(uint32_t a, uint32_t b) {  // (a NaN is passed over: it shows in the sums)
+  __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+
+// ---- sorted lists of a warp: lane i holds the i-th largest value
+template <class T>
+__device__ __forceinline__ T bitonic_step(T v, int j, bool keep_max) {
+  const T o = __shfl_xor_sync(0xffffffffu, v, j);
+  return (keep_max == (v > o)) ? v : o;  // (equal values: either)
+}
+template <class T>
+__device__ __forceinline__ T warp_sort_desc(T v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) v = bitonic_step(v, j, ((lane & j) == 0) == ((lane & k) == 0 || k == 32));
+  return v;
+}
+// the 32 largest of two sorted lists (b given in reverse: lane i holds its (31 - i)-th), sorted
+template <class T>
+__device__ __forceinline__ T warp_merge_desc(T a, T b_rev) {
+  const int lane = threadIdx.x & 31;
+  T v = a > b_rev ? a : b_rev;
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) v = bitonic_step(v, j, (lane & j) == 0);
+  return v;
+}
+// merge the warps' sorted lists into warp 0's (every thread calls)
+template <class T>
+__device__ __forceinline__ T block_merge_desc(T v, T* sm) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+  for (int half = kLpWarps / 2; half > 0; half >>= 1) {
+    __syncthreads();
+    if (warp >= half && warp < 2 * half) sm[(warp - half) * 32 + lane] = v;
+    __syncthreads();
+    if (warp < half) v = warp_merge_desc(v, sm[warp * 32 + 31 - lane]);
+  }
+  return v;
+}
+
+template <bool BF16>
+struct Row;
+template <>
+struct Row<true> {
+  static constexpr int kPer = 8;  // logits of a 16-byte vector
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
+  static __device__ __forceinline__ uint32_t up(uint32_t x, uint32_t ff) {  // (a NaN stays one)
+    __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&x), *reinterpret_cast<__nv_bfloat162*>(&ff));
+    return *reinterpret_cast<uint32_t*>(&r);
+  }
+  static __device__ __forceinline__ uint4 clamp(uint4 x, float floor) {
+    const uint32_t f = __float_as_uint(floor), ff = f | (f >> 16);
+    return make_uint4(up(x.x, ff), up(x.y, ff), up(x.z, ff), up(x.w, ff));
+  }
+  static __device__ __forceinline__ float max_of(const uint4 (&x)[kLpUnroll]) {
+    uint32_t m = hmax2(hmax2(x[0].x, x[0].y), hmax2(x[0].z, x[0].w));
+#pragma unroll
+    for (int u = 1; u < kLpUnroll; ++u) m = hmax2(m, hmax2(hmax2(x[u].x, x[u].y), hmax2(x[u].z, x[u].w)));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ void values(const uint4& x, float (&f)[kPer]) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
   }
-  if (!skip) {
-    for (int v = threadIdx.x; v < P.V; v += kLpThreads) {
-      const float d = (load_logit(P.logits, P.dtype, base + v) - m) * P.inv_t;
-      const float e = expf(d);
+};
+template <>
+struct Row<false> {
+  static constexpr int kPer = 4;
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+  // (a NaN stays one)
+  static __device__ __forceinline__ uint32_t up(uint32_t x, float floor) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(x)), "f"(floor));
+    return __float_as_uint(r);
+  }
+  static __device__ __forceinline__ uint4 clamp(uint4 x, float floor) {
+    return make_uint4(up(x.x, floor), up(x.y, floor), up(x.z, floor), up(x.w, floor));
+  }
+  static __device__ __forceinline__ float max_of(const uint4 (&x)[kLpUnroll]) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u)
+      m = max3(max3(m, __uint_as_float(x[u].x), __uint_as_float(x[u].y)), __uint_as_float(x[u].z), __uint_as_float(x[u].w));
+    return m;
+  }
+  static __device__ __forceinline__ void values(const uint4& x, float (&f)[kPer]) {
+    f[0] = __uint_as_float(x.x); f[1] = __uint_as_float(x.y); f[2] = __uint_as_float(x.z); f[3] = __uint_as_float(x.w);
+  }
+};
+
+struct LpShared {
+  float red[3 * kLpWarps];
+  float maxima[4 * 32];
+  u64 lists[4 * 32];
+  int groups[kLpThreads];
+  int n_groups, last;
+};
+
+// Sums over the block of (reference, s, w) triples of the warps, moved to the block's maximum M of the logits
+__device__ __forceinline__ void block_sums(LpShared& sm, float scale2, float r, float& s, float& w, float& M) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, off);
+    w += __shfl_xor_sync(0xffffffffu, w, off);
+  }
+  M = lp_warp_max(M);
+  const float d = (r - M) * scale2, f = lp_ex2(d);  // a warp's reference lies at most 2^8 below its maximum, and never above
+  if (lane == 0) {
+    sm.red[warp] = M;
+    sm.red[kLpWarps + warp] = s * f;
+    sm.red[2 * kLpWarps + warp] = s > 0.f || s != s ? f * fmaf(d, s, w) : 0.f;
+  }
+  __syncthreads();
+  float m = sm.red[0];
+#pragma unroll
+  for (int i = 1; i < kLpWarps; ++i) m = fmaxf(m, sm.red[i]);
+  s = w = 0.f;
+#pragma unroll
+  for (int i = 0; i < kLpWarps; ++i) {
+    const float di = (sm.red[i] - m) * scale2, fi = lp_ex2(di), si = sm.red[kLpWarps + i];
+    s = fmaf(si, fi, s);
+    if (fi > 0.f || fi != fi) w = fmaf(fi, fmaf(di, si, sm.red[2 * kLpWarps + i]), w);
+  }
+  M = m;
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const LogprobsParams P) {
+  using R = Row<BF16>;
+  __shared__ LpShared sm;
+  const int entry = blockIdx.x, piece = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tok = P.tokens[entry];
+  const int64_t row = P.rows ? P.rows[entry] : entry;
+  uint32_t why = 0;
+  if (tok >= 0 && (tok >= P.V || row < 0 || row >= P.logits_rows)) why = ISD_ST_BAD_TOKEN_ID;
+  if (tok < 0 || why) {
+    if (piece == 0) {
+      if (tid == 0) {
+        if (why) atomicOr(P.global_status, why);
+        P.logprob[entry] = NAN;
+        if (P.entropy) P.entropy[entry] = NAN;
+      }
+      if (tid < P.top_n) {
+        P.top_id[(size_t)entry * P.top_n + tid] = -1;
+        P.top_logprob[(size_t)entry * P.top_n + tid] = NAN;
+      }
+    }
+    return;
+  }
+  const int n_vec = P.V / R::kPer, per = (n_vec + P.pieces - 1) / P.pieces;
+  const int begin = min(piece * per, n_vec), end = min(begin + per, n_vec);
+  const size_t row_at = (size_t)row * P.V;
+  const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(P.logits) + row_at * (BF16 ? 2 : 4));
+  auto load = [&](int v) { return v < end ? ld_stream_16B(src + v) : R::none(); };
+
+  // ---- the pass
+  float r = -INFINITY, mine = -INFINITY;  // the warp's reference; this thread's maximum
+  uint64_t s2 = 0, w2 = 0;
+  uint4 x[kLpUnroll];
+#pragma unroll
+  for (int u = 0; u < kLpUnroll; ++u) x[u] = load(begin + tid + u * kLpThreads);
+  const uint64_t c2 = pack2(P.scale2, P.scale2);
+  uint64_t nr2 = 0;
+  for (int v = begin + tid; v - tid < end; v += kLpUnroll * kLpThreads) {
+    uint4 next[kLpUnroll];
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) next[u] = load(v + (kLpUnroll + u) * kLpThreads);
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) x[u] = R::clamp(x[u], P.floor);
+    const float m = R::max_of(x);
+    mine = fmaxf(mine, m);
+    if (__any_sync(0xffffffffu, (m - r) * P.scale2 > 8.f)) {
+      const float up = fmaxf(lp_warp_max(m), r);
+      if (r > -INFINITY) {
+        const float d = fmaxf((r - up) * P.scale2, -1000.f), f = lp_ex2(d);  // (2^-1000 is 0, and 0 * d * s has to be)
+        w2 = mul2(fma2(pack2(d, d), s2, w2), pack2(f, f));
+        s2 = mul2(s2, pack2(f, f));
+      }
+      r = up;
+      nr2 = pack2(-r, -r);
+    }
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) {
+      if (v + u * kLpThreads < end) {
+        float f[R::kPer];
+        R::values(x[u], f);
+#pragma unroll
+        for (int i = 0; i < R::kPer; i += 2) {
+          const uint64_t t = mul2(add2(pack2(f[i], f[i + 1]), nr2), c2);  // (x - r is exact where it matters, x c - r c is not)
+          float a, b;
+          unpack2(t, a, b);
+          const uint64_t e = pack2(lp_ex2(a), lp_ex2(b));
+          s2 = add2(s2, e);
+          w2 = fma2(e, t, w2);
+        }
+      }
+      x[u] = next[u];
+    }
+  }
+  float s, w, M = mine;
+  {
+    float a, b;
+    unpack2(s2, a, b);
+    s = a + b;
+    unpack2(w2, a, b);
+    w = a + b;
+  }
+  block_sums(sm, P.scale2, r, s, w, M);
+
+  // ---- alternatives of the piece
+  u64 list = 0;
+  if (P.top_n > 0) {
+    const float top = block_merge_desc(warp_sort_desc(mine), sm.maxima);
+    __syncthreads();
+    if (tid == P.top_n - 1) sm.red[0] = top <= P.floor ? -INFINITY : top;  // (what lies below the floor was held equal to it)
+    if (tid == 0) sm.n_groups = 0;
+    __syncthreads();
+    const float least = sm.red[0];
+    if (mine >= least) sm.groups[atomicAdd(&sm.n_groups, 1)] = tid;
+    __syncthreads();
+    const int groups = sm.n_groups, steps = (end - begin + kLpThreads - 1) / kLpThreads;
+    u64 bar = 0;  // the list's top_n-th key
+    for (int g = warp; g < groups; g += kLpWarps) {
+      const int first = begin + sm.groups[g];
+      for (int k0 = 0; k0 < steps; k0 += 32) {
+        const int v = first + (k0 + lane) * kLpThreads;
+        const bool in = k0 + lane < steps && v < end;
+        float f[R::kPer];
+        R::values(in ? src[v] : R::none(), f);
+#pragma unroll
+        for (int i = 0; i < R::kPer; ++i) {
+          const u64 key = lp_key(f[i], v * R::kPer + i);
+          uint32_t found = __ballot_sync(0xffffffffu, in && f[i] >= least && key > bar);
+          while (found) {
+            const int l = __ffs(found) - 1;
+            found &= found - 1;
+            const u64 k = __shfl_sync(0xffffffffu, key, l);
+            if (k <= bar) continue;
+            const int at = __popc(__ballot_sync(0xffffffffu, list > k));
+            const u64 left = __shfl_up_sync(0xffffffffu, list, 1);
+            list = lane < at ? list : (lane == at ? k : left);
+            bar = __shfl_sync(0xffffffffu, list, P.top_n - 1);
+          }
+        }
+      }
+    }
+    list = block_merge_desc(list, sm.lists);
+  }
+
+  // ---- pieces of a row meet at the last one to finish
+  if (P.pieces > 1) {
+    LpPart* part = P.part + (size_t)entry * P.pieces;
+    if (tid == 0) {
+      part[piece].m = M;
+      part[piece].s = s;
+      part[piece].w = w;
+    }
+    if (tid < P.top_n) part[piece].key[tid] = list;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) sm.last = atomicAdd(P.ticket + entry, 1) == P.pieces - 1;
+    __syncthreads();
+    if (!sm.last) return;
+    __threadfence();
+    if (tid == 0) P.ticket[entry] = 0;
+    M = -INFINITY;
+    for (int i = 0; i < P.pieces; ++i) M = fmaxf(M, __ldcg(&part[i].m));
+    s = w = 0.f;
+    for (int i = 0; i < P.pieces; ++i) {
+      const float d = (__ldcg(&part[i].m) - M) * P.scale2, f = lp_ex2(d), si = __ldcg(&part[i].s);
+      s = fmaf(si, f, s);
+      if (f > 0.f || f != f) w = fmaf(f, fmaf(d, si, __ldcg(&part[i].w)), w);
+    }
+    if (P.top_n > 0) {
+      list = 0;
+      for (int i = warp; i < P.pieces; i += kLpWarps)
+        list = warp_merge_desc(list, 31 - lane < P.top_n ? __ldcg(&part[i].key[31 - lane]) : 0ull);
+      list = block_merge_desc(list, sm.lists);
+    }
+  }
+
+  // ---- results
+  constexpr int kType = BF16 ? ISD_LOGITS_BF16 : ISD_LOGITS_F32;
+  if (M <= P.floor) {  // nothing above the floor: the pass held all of it equal, so once more, logit by logit
+    auto block_of = [&](float v, auto op) {
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, off));
+      __syncthreads();
+      if (lane == 0) sm.red[warp] = v;
+      __syncthreads();
+      v = sm.red[0];
+#pragma unroll
+      for (int i = 1; i < kLpWarps; ++i) v = op(v, sm.red[i]);
+      return v;
+    };
+    const bool seen_nan = !(s < INFINITY);
+    M = -INFINITY;
+    for (int v = tid; v < P.V; v += kLpThreads) M = fmaxf(M, load_logit(P.logits, kType, row_at + v));
+    M = block_of(M, [](float a, float b) { return fmaxf(a, b); });
+    s = w = 0.f;
+    for (int v = tid; v < P.V; v += kLpThreads) {
+      const float d = (load_logit(P.logits, kType, row_at + v) - M) * P.scale2, e = lp_ex2(d);  // (only -inf: NaN)
       s += e;
       if (e > 0.f) w = fmaf(e, d, w);
     }
-    auto add = [](float a, float b) { return a + b; };
-    s = block_reduce(s, smf, add);
-    w = block_reduce(w, smf, add);
+    s = block_of(s, [](float a, float b) { return a + b; });
+    w = block_of(w, [](float a, float b) { return a + b; });
+    if (seen_nan) s = NAN;
   }
+  const bool fine = s < INFINITY;  // a NaN or +inf among the logits shows in the sum
   const float ls = logf(s);
-  if (threadIdx.x == 0) {
-    if (why) atomicOr(P.global_status, why);
-    P.logprob[i] = skip ? NAN : (load_logit(P.logits, P.dtype, base + tok) - m) * P.inv_t - ls;
-    if (P.entropy) P.entropy[i] = skip ? NAN : ls - w / s;
+  auto logp = [&](float l) { return (l - M) * P.inv_t - ls; };
+  if (tid == 0) {
+    if (!fine) atomicOr(P.global_status, ISD_ST_NONFINITE_LOGIT);
+    P.logprob[entry] = fine ? logp(load_logit(P.logits, kType, row_at + tok)) : NAN;
+    if (P.entropy) P.entropy[entry] = fine ? ls - w / s * 0.6931471805599453f : NAN;
   }
-  unsigned long long last = ~0ull;
-  for (int k = 0; k < P.top_n; ++k) {
-    unsigned long long best = 0;
-    if (!skip)
-      for (int v = threadIdx.x; v < P.V; v += kLpThreads) {
-        const unsigned long long key =
-            ((unsigned long long)order_code(load_logit(P.logits, P.dtype, base + v)) << 32) | (0xFFFFFFFFu - (uint32_t)v);
-        if (key < last && key > best) best = key;
-      }
-    best = block_reduce(best, smk, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
-    last = best;
-    if (threadIdx.x == 0) {
-      const int id = (int)(0xFFFFFFFFu - (uint32_t)best);
-      P.top_id[(size_t)i * P.top_n + k] = skip ? -1 : id;
-      P.top_logprob[(size_t)i * P.top_n + k] = skip ? NAN : (load_logit(P.logits, P.dtype, base + id) - m) * P.inv_t - ls;
-    }
+  if (tid < P.top_n) {
+    P.top_id[(size_t)entry * P.top_n + tid] = fine ? (int)(0xFFFFFFFFu - (uint32_t)list) : -1;
+    P.top_logprob[(size_t)entry * P.top_n + tid] = fine ? logp(order_value((uint32_t)(list >> 32))) : NAN;
   }
 }
 
 }  // namespace
 
-int isd_logprobs_create(isd_ctx*) { return ISD_OK; }
-void isd_logprobs_destroy(isd_ctx*) {}
+int isd_logprobs_create(isd_ctx* ctx) {
+  LpPart* part = nullptr;
+  if (cudaMalloc(&part, sizeof(LpPart) * kLpMaxParts) != cudaSuccess) return ISD_ERR_NO_MEMORY;
+  ctx->lp_part = part;
+  if (cudaMalloc(&ctx->lp_ticket, sizeof(int) * kLpMaxParts) != cudaSuccess) return ISD_ERR_NO_MEMORY;
+  return cudaMemset(ctx->lp_ticket, 0, sizeof(int) * kLpMaxParts) == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
+}
+void isd_logprobs_destroy(isd_ctx* ctx) {
+  cudaFree(ctx->lp_part);
+  cudaFree(ctx->lp_ticket);
+}
 
 int isd_launch_logprobs(isd_ctx* ctx, const isd_logprobs_args* a, cudaStream_t stream) {
   LogprobsParams P;
-  P.logits = a->logits; P.logits_rows = a->logits_rows; P.rows = a->rows; P.tokens = a->tokens; P.n = a->n;
-  P.V = ctx->cfg.vocab; P.top_n = a->top_n; P.dtype = ctx->cfg.logits_dtype; P.inv_t = ctx->cfg.inv_temperature;
+  P.logits = a->logits; P.logits_rows = a->logits_rows; P.rows = a->rows; P.tokens = a->tokens;
+  P.V = ctx->cfg.vocab; P.top_n = a->top_n; P.inv_t = ctx->cfg.inv_temperature;
+  P.scale2 = P.inv_t * 1.4426950408889634f;
+  // (a bf16 number, so that both types are held to the same one)
+  const float floor = -1.0e36f / (P.scale2 > 1.f ? P.scale2 : 1.f);
+  uint32_t bits;
+  memcpy(&bits, &floor, sizeof(bits));
+  bits &= 0xFFFF0000u;
+  memcpy(&P.floor, &bits, sizeof(bits));
   P.logprob = a->logprob; P.entropy = a->entropy; P.top_id = a->top_id; P.top_logprob = a->top_logprob;
   P.global_status = ctx->global_status;
-  const cudaError_t e = isd_launch_pdl(logprobs_kernel, dim3(a->n), dim3(kLpThreads), 0, stream, P);
+  P.part = (LpPart*)ctx->lp_part; P.ticket = ctx->lp_ticket;
+  // rows are cut until the machine is full, but not below 4096 logits a piece
+  const int full = ctx->num_sms * kLpPerSm;
+  int pieces = full / a->n;
+  const int most = P.V / 4096;
+  pieces = pieces < most ? pieces : most;
+  pieces = pieces < kLpMaxPieces ? pieces : kLpMaxPieces;
+  P.pieces = pieces > 1 && (int64_t)pieces * a->n <= kLpMaxParts ? pieces : 1;
+  const dim3 grid(a->n, P.pieces);
+  const cudaError_t e = ctx->cfg.logits_dtype == ISD_LOGITS_BF16 ? isd_launch_pdl(logprobs_kernel<true>, grid, dim3(kLpThreads), 0, stream, P)
+                                                                 : isd_launch_pdl(logprobs_kernel<false>, grid, dim3(kLpThreads), 0, stream, P);
   ctx->launches++;
   return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }
