@@ -5,11 +5,11 @@
 // The reference is a warp's: it is raised only when a logit passes it by more than 2^8, which after the first few vectors
 // hardly happens, so the loop has no other reduction in it.
 //
-// Top alternatives without a test per element: the pass keeps each thread's maximum (which the reference needs anyway).  The
-// top_n-th largest of the 256 maxima is a lower bound of the row's top_n-th value, and only threads whose maximum reaches it
-// can hold an alternative: their elements (top_n of 256 columns of the row, still in L2) are looked at again, by warps that
-// keep a sorted list, one key per lane.  Ties go to the lower index through the key (order-preserving code of the value,
-// complement of the index).
+// Top alternatives without a test per element: the pass takes the maximum of a thread's next 64 bytes (which the reference
+// needs anyway) and leaves it in shared memory.  The top_n-th largest of the 256 threads' maxima is a lower bound of the row's
+// top_n-th value, and only 64-byte groups whose maximum reaches it can hold an alternative: little more than top_n of them,
+// which are read again (from L2) by warps that keep a sorted list, one key per lane.  Ties go to the lower index through the
+// key (order-preserving code of the value, complement of the index).
 //
 // Bound: HBM (a row is read once; 12 logits a cycle and SM at the measured copy rate), 5 instructions and one exponential a
 // logit.  Few rows are cut into pieces, whose partial results the last piece to finish merges.
@@ -165,12 +165,15 @@ struct Row<false> {
   }
 };
 
+constexpr int kLpSlots = 20;       // maxima a thread keeps; rows of more steps share them
+
 struct LpShared {
   float red[3 * kLpWarps];
   float maxima[4 * 32];
   u64 lists[4 * 32];
-  int groups[kLpThreads];
   int n_groups, last;
+  float group_max[kLpSlots][kLpThreads];
+  int groups[kLpSlots * kLpThreads];
 };
 
 // Sums over the block of (reference, s, w) triples of the warps, moved to the block's maximum M of the logits
@@ -205,7 +208,8 @@ __device__ __forceinline__ void block_sums(LpShared& sm, float scale2, float r, 
 template <bool BF16>
 __global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const LogprobsParams P) {
   using R = Row<BF16>;
-  __shared__ LpShared sm;
+  extern __shared__ __align__(16) uint8_t lp_smem[];
+  LpShared& sm = *reinterpret_cast<LpShared*>(lp_smem);
   const int entry = blockIdx.x, piece = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
   pdl_launch_dependents();
@@ -241,6 +245,10 @@ __global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const Lo
   for (int u = 0; u < kLpUnroll; ++u) x[u] = load(begin + tid + u * kLpThreads);
   const uint64_t c2 = pack2(P.scale2, P.scale2);
   uint64_t nr2 = 0;
+  // steps that share a slot of group maxima
+  const int steps = (end - begin + kLpUnroll * kLpThreads - 1) / (kLpUnroll * kLpThreads), share = (steps + kLpSlots - 1) / kLpSlots;
+  float slot_max = -INFINITY;
+  int slot = 0, left = share;
   for (int v = begin + tid; v - tid < end; v += kLpUnroll * kLpThreads) {
     uint4 next[kLpUnroll];
 #pragma unroll
@@ -249,6 +257,12 @@ __global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const Lo
     for (int u = 0; u < kLpUnroll; ++u) x[u] = R::clamp(x[u], P.floor);
     const float m = R::max_of(x);
     mine = fmaxf(mine, m);
+    slot_max = fmaxf(slot_max, m);
+    if (--left == 0) {
+      sm.group_max[slot++][tid] = slot_max;
+      slot_max = -INFINITY;
+      left = share;
+    }
     if (__any_sync(0xffffffffu, (m - r) * P.scale2 > 8.f)) {
       const float up = fmaxf(lp_warp_max(m), r);
       if (r > -INFINITY) {
@@ -277,6 +291,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const Lo
       x[u] = next[u];
     }
   }
+  if (left != share) sm.group_max[slot++][tid] = slot_max;
   float s, w, M = mine;
   {
     float a, b;
@@ -296,31 +311,35 @@ __global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const Lo
     if (tid == 0) sm.n_groups = 0;
     __syncthreads();
     const float least = sm.red[0];
-    if (mine >= least) sm.groups[atomicAdd(&sm.n_groups, 1)] = tid;
+    for (int k = 0; k < slot; ++k)
+      if (sm.group_max[k][tid] >= least) sm.groups[atomicAdd(&sm.n_groups, 1)] = k * kLpThreads + tid;
     __syncthreads();
-    const int groups = sm.n_groups, steps = (end - begin + kLpThreads - 1) / kLpThreads;
+    // a group is share * kLpUnroll vectors, kLpThreads apart; a lane takes one vector at a time
+    const int each = share * kLpUnroll, total = sm.n_groups * each;
     u64 bar = 0;  // the list's top_n-th key
-    for (int g = warp; g < groups; g += kLpWarps) {
-      const int first = begin + sm.groups[g];
-      for (int k0 = 0; k0 < steps; k0 += 32) {
-        const int v = first + (k0 + lane) * kLpThreads;
-        const bool in = k0 + lane < steps && v < end;
-        float f[R::kPer];
-        R::values(in ? src[v] : R::none(), f);
+    for (int i0 = warp * 32; i0 < total; i0 += kLpThreads) {
+      const int i = i0 + lane;
+      int v = end;
+      if (i < total) {
+        const int g = sm.groups[i / each];
+        v = begin + (g / kLpThreads * each + i % each) * kLpThreads + g % kLpThreads;
+      }
+      const bool in = v < end;
+      float f[R::kPer];
+      R::values(in ? src[v] : R::none(), f);
 #pragma unroll
-        for (int i = 0; i < R::kPer; ++i) {
-          const u64 key = lp_key(f[i], v * R::kPer + i);
-          uint32_t found = __ballot_sync(0xffffffffu, in && f[i] >= least && key > bar);
-          while (found) {
-            const int l = __ffs(found) - 1;
-            found &= found - 1;
-            const u64 k = __shfl_sync(0xffffffffu, key, l);
-            if (k <= bar) continue;
-            const int at = __popc(__ballot_sync(0xffffffffu, list > k));
-            const u64 left = __shfl_up_sync(0xffffffffu, list, 1);
-            list = lane < at ? list : (lane == at ? k : left);
-            bar = __shfl_sync(0xffffffffu, list, P.top_n - 1);
-          }
+      for (int e = 0; e < R::kPer; ++e) {
+        const u64 key = lp_key(f[e], v * R::kPer + e);
+        uint32_t found = __ballot_sync(0xffffffffu, in && f[e] >= least && key > bar);
+        while (found) {
+          const int l = __ffs(found) - 1;
+          found &= found - 1;
+          const u64 k = __shfl_sync(0xffffffffu, key, l);
+          if (k <= bar) continue;
+          const int at = __popc(__ballot_sync(0xffffffffu, list > k));
+          const u64 before = __shfl_up_sync(0xffffffffu, list, 1);
+          list = lane < at ? list : (lane == at ? k : before);
+          bar = __shfl_sync(0xffffffffu, list, P.top_n - 1);
         }
       }
     }
@@ -437,8 +456,8 @@ int isd_launch_logprobs(isd_ctx* ctx, const isd_logprobs_args* a, cudaStream_t s
   pieces = pieces < kLpMaxPieces ? pieces : kLpMaxPieces;
   P.pieces = pieces > 1 && (int64_t)pieces * a->n <= kLpMaxParts ? pieces : 1;
   const dim3 grid(a->n, P.pieces);
-  const cudaError_t e = ctx->cfg.logits_dtype == ISD_LOGITS_BF16 ? isd_launch_pdl(logprobs_kernel<true>, grid, dim3(kLpThreads), 0, stream, P)
-                                                                 : isd_launch_pdl(logprobs_kernel<false>, grid, dim3(kLpThreads), 0, stream, P);
+  const cudaError_t e = ctx->cfg.logits_dtype == ISD_LOGITS_BF16 ? isd_launch_pdl(logprobs_kernel<true>, grid, dim3(kLpThreads), sizeof(LpShared), stream, P)
+                                                                 : isd_launch_pdl(logprobs_kernel<false>, grid, dim3(kLpThreads), sizeof(LpShared), stream, P);
   ctx->launches++;
   return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }
