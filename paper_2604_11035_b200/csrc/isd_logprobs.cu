@@ -6,7 +6,7 @@
 // hardly happens, so the loop has no other reduction in it.
 //
 // Top alternatives without a test per element: the pass takes the maximum of a thread's next 64 bytes (which the reference
-// needs anyway) and leaves it in shared memory.  The top_n-th largest of the 256 threads' maxima is a lower bound of the row's
+// needs anyway) and leaves it in shared memory.  The top_n-th largest of the threads' maxima is a lower bound of the row's
 // top_n-th value, and only 64-byte groups whose maximum reaches it can hold an alternative: little more than top_n of them,
 // which are read again (from L2) by warps that keep a sorted list, one key per lane.  Ties go to the lower index through the
 // key (order-preserving code of the value, complement of the index).
@@ -19,9 +19,9 @@
 
 namespace {
 
-constexpr int kLpThreads = 256;
+constexpr int kLpThreads = 128;     // small CTAs: one merges and ranks at the end of its row while five others stream
 constexpr int kLpWarps = kLpThreads / 32;
-constexpr int kLpPerSm = 4;        // resident CTAs
+constexpr int kLpPerSm = 6;        // resident CTAs (4 x 256 threads: the same at 2048 rows, a quarter slower at 777)
 constexpr int kLpMaxPieces = 32;
 constexpr int kLpMaxParts = 4096;  // pieces of all rows of a call that cuts them
 constexpr int kLpUnroll = 4;       // 16-byte vectors a thread has in flight, twice
