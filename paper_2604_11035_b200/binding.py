@@ -81,6 +81,8 @@ class IsdLogprobsArgs(C.Structure):
         [(n, C.c_void_p) for n in ("logprob", "entropy", "top_id", "top_logprob")]
 
 
+_STATE_FIELDS = [n for n, _ in IsdBatchState._fields_]
+
 _lib = None
 
 
@@ -176,32 +178,43 @@ def _ptr(t):
     if t is None:
         return None
     assert t.is_cuda and t.is_contiguous(), "device, contiguous tensors only"
-    return t.data_ptr() if t.numel() > 0 else None
+    return t.data_ptr() or None  # (a tensor without elements has no address)
 
 
 def _arg(t, name, dtype, shape, device):
-    """Device pointer of a dense tensor argument that has to have this dtype and shape; None passes as NULL."""
+    """Device pointer of a dense tensor argument that has to have this dtype and shape (a tuple) and be on device `device` (an
+    index); None passes as NULL.  Small calls are bound by the host: the checks are attribute reads and nothing else."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) \
-            or not t.is_contiguous():
-        got = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
-        raise IsdError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {got}")
-    return t.data_ptr() if t.numel() > 0 else None
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr() or None
+        got = f"{t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous")
+    except AttributeError:
+        got = type(t).__name__
+    raise IsdError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}, got {got}")
 
 
-def _rows_arg(t, name, rows, heads, device):
+def _rows_arg(t, name, shape, device):
     """(device pointer, row stride in elements) of bf16 rows [rows, heads, 128] that are dense within a row."""
-    if t.device != device or t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, heads, 128):
-        raise IsdError(f"{name}: expected a bf16 tensor of shape {(rows, heads, 128)} on {device}, "
-                       f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    stride = heads * 128 if rows <= 1 else t.stride(0)
-    if rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128) or stride < heads * 128 or stride % 8):
+    if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != device:
+        raise IsdError(f"{name}: expected a bf16 tensor of shape {shape} on cuda:{device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    rows, row = shape[0], shape[1] * 128
+    stride, head, dim = t.stride()
+    if rows <= 1:
+        stride = row
+    if rows and (dim != 1 or (head != 128 and shape[1] > 1) or stride < row or stride % 8):
         raise IsdError(f"{name}: rows have to be dense and a multiple of 8 elements apart, got strides {t.stride()}")
-    return (t.data_ptr() if rows else None), stride
+    return t.data_ptr() or None, stride
+
+
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream():
+    if _raw_stream is not None:  # the handle alone, without a Stream object around it
+        return _raw_stream(_current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -252,6 +265,7 @@ class Isd:
             raise IsdError("a CUDA device is required (there is no CPU path)")
         self.lib = load()
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._dev = self.device.index
         ld = {"f32": 0, "bf16": 1, torch.float32: 0, torch.bfloat16: 1, 0: 0, 1: 1}[logits_dtype]
         self.cfg = IsdConfig(batch, stride, n_q_heads, n_kv_heads, head_dim, page_size, vocab,
                              max_pages_per_slot, num_pages, ld, q_mode, propose_mode,
@@ -260,6 +274,9 @@ class Isd:
         self.ctx = C.c_void_p()
         _check(self.lib.isd_create(C.byref(self.cfg), C.byref(self.ctx)), "isd_create")
         self.N, self.B = stride, batch
+        rows = (batch, 2 * stride - 1)
+        self._q_shape, self._kv_shape = (*rows, n_q_heads, 128), (*rows, n_kv_heads, 128)
+        self._lse_shape, self._pool_shape = (*rows, n_q_heads), (num_pages, n_kv_heads, QUANT_TILE_BYTES)
 
     def close(self):
         if getattr(self, "ctx", None) and self.ctx.value:
@@ -275,7 +292,7 @@ class Isd:
     # -- struct marshalling
     @staticmethod
     def state_struct(st: dict) -> IsdBatchState:
-        return IsdBatchState(*[_ptr(st[n]) for n, _ in IsdBatchState._fields_])
+        return IsdBatchState(*[_ptr(st[n]) for n in _STATE_FIELDS])
 
     @staticmethod
     def out_struct(out: dict) -> IsdVerifyOut:
@@ -331,14 +348,10 @@ class Isd:
         return y
 
     def _quant_ptrs(self, q, k_new, v_new, kv_pool, attn_out, attn_lse):
-        c, bf, Q = self.cfg, torch.bfloat16, 2 * self.N - 1
-        row, kv = (self.B, Q, c.n_q_heads, 128), (self.B, Q, c.n_kv_heads, 128)
-        return [_arg(q, "q", bf, row, self.device), _arg(k_new, "k_new", bf, kv, self.device),
-                _arg(v_new, "v_new", bf, kv, self.device), self._pool_ptr(kv_pool),
-                _arg(attn_out, "attn_out", bf, row, self.device), _arg(attn_lse, "attn_lse", torch.float32, row[:3], self.device)]
-
-    def _pool_ptr(self, kv_pool):
-        return _arg(kv_pool, "kv_pool", torch.uint8, (self.cfg.num_pages, self.cfg.n_kv_heads, QUANT_TILE_BYTES), self.device)
+        bf, dev = torch.bfloat16, self._dev
+        return (_arg(q, "q", bf, self._q_shape, dev), _arg(k_new, "k_new", bf, self._kv_shape, dev),
+                _arg(v_new, "v_new", bf, self._kv_shape, dev), _arg(kv_pool, "kv_pool", torch.uint8, self._pool_shape, dev),
+                _arg(attn_out, "attn_out", bf, self._q_shape, dev), _arg(attn_lse, "attn_lse", torch.float32, self._lse_shape, dev))
 
     def isd_attn_quant(self, st, q, k_new, v_new, kv_pool, attn_out, attn_lse=None):
         """isd_attn over the 4-bit cache `kv_pool` (uint8 [num_pages, Hkv, 2176], see alloc_kv_pool_quant)."""
@@ -362,10 +375,11 @@ class Isd:
                                        C.byref(o), step, _stream()), "isd_step_quant")
 
     def _kv_quant_args(self, k, v, slot_map, kv_pool):
-        n, h = slot_map.numel(), self.cfg.n_kv_heads
-        (kp, ks), (vp, vs) = _rows_arg(k, "k", n, h, self.device), _rows_arg(v, "v", n, h, self.device)
-        return IsdKvQuantArgs(kp, vp, ks, vs, _arg(slot_map, "slot_map", torch.int64, (n,), self.device),
-                              self._pool_ptr(kv_pool), n)
+        n, dev = slot_map.numel(), self._dev
+        shape = (n, self.cfg.n_kv_heads, 128)
+        (kp, ks), (vp, vs) = _rows_arg(k, "k", shape, dev), _rows_arg(v, "v", shape, dev)
+        return IsdKvQuantArgs(kp, vp, ks, vs, _arg(slot_map, "slot_map", torch.int64, (n,), dev),
+                              _arg(kv_pool, "kv_pool", torch.uint8, self._pool_shape, dev), n)
 
     def isd_kv_write_quant(self, k, v, slot_map, kv_pool):
         """Quantise rows k, v [T, Hkv, 128] bf16 (rows may be strided) into the slots of slot_map [T] int64 (< 0: skipped)."""
@@ -380,7 +394,7 @@ class Isd:
     def isd_admit(self, st, slots, lens, anchors, maps):
         """Admit requests (slot, cached length, anchor token: int32 [n]) into inactive slots; `maps`: see alloc_admit_maps
         (slot_map, tok_req, tok_pos may be None)."""
-        n, i32, dev = slots.numel(), torch.int32, self.device
+        n, i32, dev = slots.numel(), torch.int32, self._dev
         some = next((maps[k] for k in ("slot_map", "tok_req", "tok_pos") if maps.get(k) is not None), None)
         cap = 0x7FFFFFFF if some is None else some.numel()
         a = IsdAdmitArgs(_arg(slots, "slots", i32, (n,), dev), _arg(lens, "lens", i32, (n,), dev),
@@ -401,7 +415,7 @@ class Isd:
         if rows is None and n > total:
             raise IsdError(f"logits: {total} rows for {n} tokens")
         out = alloc_logprobs_out(n, top_n, self.device) if out is None else out
-        i32, f32, dev = torch.int32, torch.float32, self.device
+        i32, f32, dev = torch.int32, torch.float32, self._dev
         a = IsdLogprobsArgs(_arg(logits, "logits", dt, (*logits.shape[:-1], V), dev), total, _arg(rows, "rows", i32, (n,), dev),
                             _arg(tokens, "tokens", i32, (n,), dev), n, top_n, _arg(out["logprob"], "logprob", f32, (n,), dev),
                             _arg(out.get("entropy"), "entropy", f32, (n,), dev),
