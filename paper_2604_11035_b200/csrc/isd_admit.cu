@@ -1,7 +1,7 @@
 // isd_admit: requests enter free slots (Sec. 3.3 (2): the stationary batch takes new requests without the host).
 // Pages come from the free stack in request order, by an exclusive prefix sum of what the requests ask for, so the
 // result does not depend on thread scheduling.  Two kernels: a CTA that plans and commits the state, and a grid that
-// writes the tokens' maps.
+// writes page tables and the tokens' maps.
 #include <limits.h>
 
 #include "isd_commit.cuh"
@@ -29,6 +29,9 @@ struct AdmitParams {
   uint8_t* active;
   uint32_t* slot_status;
   int* mark;
+  // plan of the call for the second kernel: [0] admitted requests, [1] free pages before the call; then of the k-th admitted
+  // request: index, pages of the admitted ones before it (one more entry: of all)
+  int* plan;
 };
 
 constexpr int kAdmitThreads = 1024;
@@ -45,7 +48,9 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
   __syncthreads();
   const int top = *P.free_top;
   int64_t pages0 = 0, toks0 = 0;  // asked for by valid requests of earlier rounds
-  int served_pages = 0, served_toks = 0;
+  int served_pages = 0, served_toks = 0, served = 0;
+  int* plan_req = P.plan + 2;
+  int* plan_page = plan_req + P.B;
   for (int base = 0; base < P.n; base += kAdmitThreads) {
     const int i = base + threadIdx.x;
     uint32_t why = 0;
@@ -75,15 +80,16 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
       else if (before_t + len > P.map_cap) why = ISD_ST_MAP_FULL;
     }
     const bool ok = asks && !why;
-    int n_p, n_t;
-    block_exclusive_scan(ok ? want : 0, sm_warp, n_p);
+    // (admitted requests are at most one per slot, so their number and the pages they take fit one scan each)
+    int n_p, n_t, n_k;
+    const int my_p = block_exclusive_scan(ok ? want : 0, sm_warp, n_p);
     const int my_t = block_exclusive_scan(ok ? len : 0, sm_warp, n_t);
+    const int my_k = served + block_exclusive_scan(ok ? 1 : 0, sm_warp, n_k);
     if (i < P.n) {
       P.result[i] = (int32_t)why;
       P.cu_len[i] = served_toks + my_t;
     }
     served_toks += n_t;
-    served_pages += n_p;
     if (ok) {
       P.ctx_len[b] = len;
       P.n_ver[b] = 0;
@@ -91,8 +97,11 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
       P.slot_status[b] = 0;
       P.active[b] = 1;
       for (int m = 0; m < P.Q; ++m) P.block_tok[(size_t)b * P.Q + m] = m == 0 ? P.anchors[i] : P.mask_token;
-      for (int j = 0; j < want; ++j) P.page_table[(size_t)b * P.max_pages + j] = P.free_stack[top - 1 - (before_p + j)];
+      plan_req[my_k] = i;
+      plan_page[my_k] = served_pages + my_p;
     }
+    served += n_k;
+    served_pages += n_p;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < P.n; i += kAdmitThreads) {
@@ -102,25 +111,52 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
   if (threadIdx.x == 0) {
     P.cu_len[P.n] = served_toks;
     *P.free_top = top - served_pages;
+    P.plan[0] = served;
+    P.plan[1] = top;
+    plan_page[served] = served_pages;
   }
 }
 
+// Page tables and maps: a half-warp per page, lane = token of the page.  The k-th page taken is free_stack[top - 1 - k]
+// whoever takes it (those served are a prefix of those who ask), so only the request of a page has to be found: by a search
+// once per kPagesEach pages, then by stepping on.
+constexpr int kPagesEach = 16;
 __global__ void __launch_bounds__(256) admit_maps_kernel(const AdmitParams P) {
   pdl_wait();
   pdl_launch_dependents();
-  const int total = P.cu_len[P.n];
-  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-    // last request whose tokens begin at or before t (requests without tokens share their successor's beginning)
-    int lo = 0, hi = P.n;
-    while (lo < hi) {
+  const int served = P.plan[0], top = P.plan[1];
+  const int* plan_req = P.plan + 2;
+  const int* plan_page = plan_req + P.B;
+  if (served == 0) return;
+  const int pages = plan_page[served], off = threadIdx.x & 15;
+  const int group = (blockIdx.x * 256 + threadIdx.x) >> 4, groups = gridDim.x * 16;
+  for (int k0 = group * kPagesEach; k0 < pages; k0 += groups * kPagesEach) {
+    int lo = 0, hi = served;  // last request whose pages begin at or before k0 (every request takes at least one)
+    while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (P.cu_len[mid + 1] > t) hi = mid; else lo = mid + 1;
+      if (plan_page[mid] <= k0) lo = mid; else hi = mid;
     }
-    const int pos = (int)t - P.cu_len[lo];
-    if (P.slot_map)
-      P.slot_map[t] = (int64_t)P.page_table[(size_t)P.slots[lo] * P.max_pages + pos / ISD_PAGE] * ISD_PAGE + pos % ISD_PAGE;
-    if (P.tok_req) P.tok_req[t] = lo;
-    if (P.tok_pos) P.tok_pos[t] = pos;
+    int first = -1, next = -1, req = 0, slot = 0, len = 0, cu = 0;
+    for (int k = k0; k < min(k0 + kPagesEach, pages); ++k) {
+      if (k >= next) {  // (also the first time)
+        if (next >= 0) ++lo;
+        first = plan_page[lo];
+        next = plan_page[lo + 1];
+        req = plan_req[lo];
+        slot = P.slots[req];
+        len = P.lens[req];
+        cu = P.cu_len[req];
+      }
+      const int j = k - first, pos = j * ISD_PAGE + off;
+      const int page = P.free_stack[top - 1 - k];
+      if (off == 0) P.page_table[(size_t)slot * P.max_pages + j] = page;
+      if (pos < len) {
+        const int t = cu + pos;
+        if (P.slot_map) P.slot_map[t] = (int64_t)page * ISD_PAGE + off;
+        if (P.tok_req) P.tok_req[t] = req;
+        if (P.tok_pos) P.tok_pos[t] = pos;
+      }
+    }
   }
 }
 
@@ -129,10 +165,14 @@ __global__ void __launch_bounds__(256) admit_maps_kernel(const AdmitParams P) {
 int isd_admit_create(isd_ctx* ctx) {
   const size_t B = (size_t)ctx->cfg.batch;
   if (cudaMalloc(&ctx->admit_mark, sizeof(int) * B) != cudaSuccess) return ISD_ERR_NO_MEMORY;
+  if (cudaMalloc(&ctx->admit_plan, sizeof(int) * (2 * B + 3)) != cudaSuccess) return ISD_ERR_NO_MEMORY;
   return cudaMemset(ctx->admit_mark, 0x7F, sizeof(int) * B) == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }
 
-void isd_admit_destroy(isd_ctx* ctx) { cudaFree(ctx->admit_mark); }
+void isd_admit_destroy(isd_ctx* ctx) {
+  cudaFree(ctx->admit_mark);
+  cudaFree(ctx->admit_plan);
+}
 
 int isd_launch_admit(isd_ctx* ctx, isd_batch_state* st, const isd_admit_args* a, cudaStream_t stream) {
   const isd_config& c = ctx->cfg;
@@ -142,11 +182,13 @@ int isd_launch_admit(isd_ctx* ctx, isd_batch_state* st, const isd_admit_args* a,
   P.slot_map = a->slot_map; P.tok_req = a->tok_req; P.tok_pos = a->tok_pos;
   P.ctx_len = st->ctx_len; P.n_ver = st->n_ver; P.block_tok = st->block_tok; P.q_row0 = st->q_row0; P.page_table = st->page_table;
   P.free_stack = st->free_stack; P.free_top = st->free_top; P.active = st->active; P.slot_status = st->slot_status;
-  P.mark = ctx->admit_mark;
+  P.mark = ctx->admit_mark; P.plan = ctx->admit_plan;
   cudaError_t e = isd_launch_pdl(admit_plan_kernel, dim3(1), dim3(kAdmitThreads), 0, stream, P);
   ctx->launches++;
-  if (e == cudaSuccess && a->n > 0 && a->map_cap > 0 && (a->slot_map || a->tok_req || a->tok_pos)) {
-    const int64_t ctas = (a->map_cap + 255) / 256;
+  if (e == cudaSuccess && a->n > 0) {
+    // pages at most: what the pool holds, and what the valid requests can ask for
+    const int64_t asked = (int64_t)(a->n < c.batch ? a->n : c.batch) * c.max_pages_per_slot, pages = asked < c.num_pages ? asked : c.num_pages;
+    const int64_t ctas = (pages + 16 * kPagesEach - 1) / (16 * kPagesEach);
     const int most = ctx->num_sms * 8;
     e = isd_launch_pdl(admit_maps_kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, stream, P);
     ctx->launches++;

@@ -246,7 +246,7 @@ static int check_kv_quant(const isd_ctx* ctx, const isd_kv_quant_args* a) {
   const int64_t row = (int64_t)ctx->cfg.n_kv_heads * ISD_HEAD_DIM;
   if (a->k_row_stride < row || a->v_row_stride < row || a->k_row_stride % 8 != 0 || a->v_row_stride % 8 != 0)
     return ISD_ERR_INVALID_ARG;
-  if (a->n_tokens > (int64_t)0x7FFFFFFF * 16 / ctx->cfg.n_kv_heads) return ISD_ERR_INVALID_ARG;
+  if (a->n_tokens > (int64_t)0x7FFFFFFF * 16) return ISD_ERR_INVALID_ARG;
   if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->kv_pool)) return ISD_ERR_ALIGNMENT;
   return ISD_OK;
 }

@@ -1,8 +1,8 @@
 // The 4-bit KV cache's traffic: the block append of isd_attn_quant, isd_kv_write_quant and isd_kv_read_quant
 // (Sec. 3.3 (2): KV rows enter the paged cache by one batched scatter).
 //
-// The latter two work on runs of consecutive tokens inside a page, one warp per (run, kv head): a V word holds eight
-// tokens of a dim, so a run's words are built in registers and stored whole.
+// The latter two work on runs of consecutive tokens inside a page: a V word holds eight tokens of a dim, so that a run's
+// words can be stored whole.
 #include "isd_quant.cuh"
 
 namespace {
@@ -123,52 +123,120 @@ struct RowsParams {
   const int64_t* slot_map;
   uint8_t* pool;
   int64_t n_tokens, n_slots;
-  int Hkv;
+  int Hkv, heads_each;  // kv heads, and how many of them a CTA takes
   uint32_t* global_status;
 };
 
-constexpr int kWindow = 16;  // tokens whose runs one warp owns
-constexpr int kRowsWarps = 4;
+constexpr int kWindow = 16;        // tokens whose runs one CTA owns
+constexpr int kRowsThreads = 256;  // a half-warp per token of a page
 
-// The runs (consecutive slots of one page at consecutive tokens) that start in a window of kWindow tokens, one warp per
-// (window, kv head): a run belongs to the window of its first token and may reach up to 15 tokens into the next one, so
-// that no page of a request is cut between two warps, wherever the window's border falls.
-template <class Body>
-__device__ __forceinline__ void for_runs(const RowsParams& P, Body body) {
-  const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * kRowsWarps + (threadIdx.x >> 5);
-  const int g = (int)(item % P.Hkv);
-  const int64_t t0 = item / P.Hkv * kWindow;
-  if (t0 >= P.n_tokens) return;
-  const int64_t t = t0 + lane;
-  int64_t slot = t < P.n_tokens ? P.slot_map[t] : -1;
-  int64_t prev = __shfl_up_sync(0xffffffffu, slot, 1);
-  if (lane == 0) prev = t0 > 0 ? P.slot_map[t0 - 1] : -1;
-  if (slot >= P.n_slots) {
-    if (g == 0 && lane < kWindow) atomicOr(P.global_status, ISD_ST_BAD_PAGE_ID);
-    slot = -1;
+// The runs (consecutive slots of one page at consecutive tokens) that start in a window of kWindow tokens: a run belongs to
+// the window of its first token and may reach up to 15 tokens into the next one, so that no page of a request is cut between
+// two CTAs, wherever the window's border falls.  Every warp of a CTA finds them for itself.
+struct Runs {
+  int64_t t0, slot;
+  uint32_t on, heads;
+  __device__ __forceinline__ void find(const RowsParams& P, int64_t t0_, bool report) {
+    const int lane = threadIdx.x & 31;
+    t0 = t0_;
+    const int64_t t = t0 + lane;
+    slot = t < P.n_tokens ? P.slot_map[t] : -1;
+    int64_t prev = __shfl_up_sync(0xffffffffu, slot, 1);
+    if (lane == 0) prev = t0 > 0 ? P.slot_map[t0 - 1] : -1;
+    if (slot >= P.n_slots) {
+      if (report && lane < kWindow) atomicOr(P.global_status, ISD_ST_BAD_PAGE_ID);
+      slot = -1;
+    }
+    // a token goes on the run before it unless it is the first of a page (prev + 1 == slot >= 1 then implies prev valid)
+    const bool goes_on = slot >= 0 && (slot & 15) != 0 && prev == slot - 1;
+    on = __ballot_sync(0xffffffffu, goes_on);
+    heads = __ballot_sync(0xffffffffu, slot >= 0 && !goes_on && lane < kWindow);
   }
-  // a token goes on the run before it unless it is the first of a page (prev + 1 == slot >= 1 then implies prev valid)
-  const bool goes_on = slot >= 0 && (slot & 15) != 0 && prev == slot - 1;
-  const uint32_t on = __ballot_sync(0xffffffffu, goes_on);
-  uint32_t heads = __ballot_sync(0xffffffffu, slot >= 0 && !goes_on && lane < kWindow);
-  while (heads) {
+  // the next run: its first token, offset in the page, length, and page
+  __device__ __forceinline__ bool next(int64_t& t, int& off, int& cnt, int64_t& page) {
+    if (!heads) return false;
     const int l = __ffs(heads) - 1;
     heads &= heads - 1;
-    const uint32_t after = l < 31 ? ~(on >> (l + 1)) : 1u;  // first token after the head that does not go on
-    const int cnt = min(__ffs(after), 32 - l);
+    const uint32_t after = ~(on >> (l + 1));  // first token after the head that does not go on (l < 16)
+    cnt = min(__ffs(after), 32 - l);
     const int64_t s = __shfl_sync(0xffffffffu, slot, l);
-    body(t0 + l, (int)(s & 15), cnt, P.pool + ((size_t)(s >> 4) * P.Hkv + g) * kQTile, g);
+    t = t0 + l;
+    off = (int)(s & 15);
+    page = s >> 4;
+    return true;
   }
-}
+};
 
-__global__ void __launch_bounds__(kRowsWarps * 32) kv_write_quant_kernel(const RowsParams P) {
+// A CTA walks the runs of a window and, for each, some of the kv heads: half-warp = token of the page, lane = eight dims.  K
+// words are complete in a lane; V words hold eight tokens of a dim and are put together through shared memory (two buffers:
+// one barrier a head).  The next head's rows are fetched before this one is encoded.
+// Bound: HBM (512 bytes in, 136 out per token and head).  As one warp per (run, head), which encoded its 16 tokens one after the
+// other, the write took twice as long.
+__global__ void __launch_bounds__(kRowsThreads) kv_write_quant_kernel(const RowsParams P) {
+  __shared__ uint2 codes[2][16][16];  // V codes, a byte each: [buffer][token][eight dims]
   pdl_wait();
   pdl_launch_dependents();
-  for_runs(P, [&](int64_t t, int off, int cnt, uint8_t* tile, int g) {
-    quant_store_run(P.k + (size_t)t * P.k_stride + g * ISD_HEAD_DIM, P.k_stride,
-                          P.v + (size_t)t * P.v_stride + g * ISD_HEAD_DIM, P.v_stride, tile, off, cnt);
-  });
+  const int hw = threadIdx.x >> 4, hl = threadIdx.x & 15;
+  const int g0 = blockIdx.y * P.heads_each, g1 = min(g0 + P.heads_each, P.Hkv);
+  Runs runs;
+  runs.find(P, (int64_t)blockIdx.x * kWindow, g0 == 0 && threadIdx.x < 32);
+  int64_t t, page;
+  int off, cnt, buf = 0;
+  while (runs.next(t, off, cnt, page)) {
+    const bool mine = hw >= off && hw < off + cnt;
+    const size_t row = (size_t)(t + (mine ? hw - off : 0));
+    const __nv_bfloat16* k = P.k + row * P.k_stride + hl * 8;
+    const __nv_bfloat16* v = P.v + row * P.v_stride + hl * 8;
+    uint4 kx = *reinterpret_cast<const uint4*>(k + (size_t)g0 * ISD_HEAD_DIM), vx = *reinterpret_cast<const uint4*>(v + (size_t)g0 * ISD_HEAD_DIM);
+    for (int g = g0; g < g1; ++g, buf ^= 1) {
+      uint8_t* tile = P.pool + ((size_t)page * P.Hkv + g) * kQTile;
+      uint4 kn = kx, vn = vx;
+      if (g + 1 < g1) {
+        kn = *reinterpret_cast<const uint4*>(k + (size_t)(g + 1) * ISD_HEAD_DIM);
+        vn = *reinterpret_cast<const uint4*>(v + (size_t)(g + 1) * ISD_HEAD_DIM);
+      }
+      const QuantParam pk = quant_half_warp(kx), pv = quant_half_warp(vx);
+      float f[8];
+      unpack8(kx, f);
+      uint32_t w = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w |= quant_code(f[e], pk) << (4 * (e >> 1) + 16 * (e & 1));
+      unpack8(vx, f);
+      uint32_t c[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e] = quant_code(f[e], pv);
+      if (mine) {
+        *reinterpret_cast<uint32_t*>(tile + (hl >> 2) * 256 + hw * 16 + (hl & 3) * 4) = w;
+        if (hl < 4)
+          reinterpret_cast<uint16_t*>(tile + kQOffMeta)[hl * 16 + hw] = hl == 0 ? pk.s_bits : (hl == 1 ? pk.z_bits : (hl == 2 ? pv.s_bits : pv.z_bits));
+      }
+      codes[buf][hw][hl] = make_uint2(c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24), c[4] | (c[5] << 8) | (c[6] << 16) | (c[7] << 24));
+      __syncthreads();
+      {  // thread = (dim, half of the page)
+        const int dim = threadIdx.x >> 1, half = threadIdx.x & 1;
+        const uint8_t* bytes = reinterpret_cast<const uint8_t*>(codes[buf]);
+        uint32_t word = 0, mask = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int tok = half * 8 + e, sh = 4 * (e >> 1) + 16 * (e & 1);
+          if (tok >= off && tok < off + cnt) {
+            word |= (uint32_t)bytes[tok * ISD_HEAD_DIM + dim] << sh;
+            mask |= 0xFu << sh;
+          }
+        }
+        uint32_t* dst = reinterpret_cast<uint32_t*>(tile + kQOffV) + threadIdx.x;
+        if (mask == 0xFFFFFFFFu) {
+          *dst = word;
+        } else if (mask) {
+          // other CTAs may be writing other tokens of the word; their nibbles are disjoint, so clearing and setting bits commutes
+          atomicAnd(dst, ~mask);
+          atomicOr(dst, word);
+        }
+      }
+      kx = kn;
+      vx = vn;
+    }
+  }
 }
 
 // bf16 pair of scale * (code - zero): the integer difference and its product with the scale are exact in fp32
@@ -177,49 +245,59 @@ __device__ __forceinline__ uint32_t value_pair(uint32_t d, float s0, float s1) {
   return as_u32(__floats2bfloat162_rn(lo, hi));
 }
 
-__global__ void __launch_bounds__(kRowsWarps * 32) kv_read_quant_kernel(const RowsParams P) {
+// The way back: the tile of a (page, head) comes into shared memory whole (two buffers; the next head's is under way), then a
+// half-warp writes its token's rows in 16-byte pieces.  Bound: HBM (136 bytes in, 512 out per token and head).
+__global__ void __launch_bounds__(kRowsThreads) kv_read_quant_kernel(const RowsParams P) {
+  constexpr int kVecs = kQTile / 16;  // 136
+  __shared__ uint4 tiles[2][kVecs];
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, hl = lane & 15, par = lane >> 4;
-  for_runs(P, [&](int64_t t0, int off, int cnt, const uint8_t* tile, int g) {
-    const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + kQOffMeta);
-    __nv_bfloat16* k = P.k + (size_t)t0 * P.k_stride + g * ISD_HEAD_DIM;
-    __nv_bfloat16* v = P.v + (size_t)t0 * P.v_stride + g * ISD_HEAD_DIM;
-    // K: half-warp per token, eight dims a lane
+  const int hw = threadIdx.x >> 4, hl = threadIdx.x & 15;
+  const int g0 = blockIdx.y * P.heads_each, g1 = min(g0 + P.heads_each, P.Hkv);
+  Runs runs;
+  runs.find(P, (int64_t)blockIdx.x * kWindow, g0 == 0 && threadIdx.x < 32);
+  int64_t t, page;
+  int off, cnt, buf = 0;
+  while (runs.next(t, off, cnt, page)) {
+    const bool mine = hw >= off && hw < off + cnt, loads = threadIdx.x < kVecs;
+    const uint4* src = reinterpret_cast<const uint4*>(P.pool + (size_t)page * P.Hkv * kQTile) + threadIdx.x;
+    const size_t row = (size_t)(t + (mine ? hw - off : 0));
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (loads) x = src[(size_t)g0 * kVecs];
+    for (int g = g0; g < g1; ++g, buf ^= 1) {
+      if (loads) tiles[buf][threadIdx.x] = x;
+      __syncthreads();
+      if (loads && g + 1 < g1) x = src[(size_t)(g + 1) * kVecs];
+      if (mine) {
+        const uint8_t* tile = reinterpret_cast<const uint8_t*>(tiles[buf]);
+        const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + kQOffMeta);
+        {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + (hl >> 2) * 256 + hw * 16 + (hl & 3) * 4);
+          const float s = bf16_bits_to_f32(meta[hw]);
+          const uint32_t z = meta[16 + hw] * 0x10001u;
+          uint4 o;
+          o.x = value_pair(sub_zero(codes_to_bf16(w), z), s, s);
+          o.y = value_pair(sub_zero(codes_to_bf16(w >> 4), z), s, s);
+          o.z = value_pair(sub_zero(codes_to_bf16(w >> 8), z), s, s);
+          o.w = value_pair(sub_zero(codes_to_bf16(w >> 12), z), s, s);
+          *reinterpret_cast<uint4*>(P.k + row * P.k_stride + (size_t)g * ISD_HEAD_DIM + hl * 8) = o;
+        }
+        {
+          const float s = bf16_bits_to_f32(meta[32 + hw]);
+          const uint32_t z = meta[48 + hw] * 0x10001u;
+          const int sh = 4 * ((hw & 7) >> 1) + 16 * (hw & 1);
+          const uint32_t* words = reinterpret_cast<const uint32_t*>(tile + kQOffV) + hl * 16 + (hw >> 3);  // [dim][2]
+          uint32_t p[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int t = 2 * i + par;
-      if (t < off || t >= off + cnt) continue;
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + (hl >> 2) * 256 + t * 16 + (hl & 3) * 4);
-      const float s = bf16_bits_to_f32(meta[t]);
-      const uint32_t z = meta[16 + t] * 0x10001u;
-      uint4 o;
-      o.x = value_pair(sub_zero(codes_to_bf16(w), z), s, s);
-      o.y = value_pair(sub_zero(codes_to_bf16(w >> 4), z), s, s);
-      o.z = value_pair(sub_zero(codes_to_bf16(w >> 8), z), s, s);
-      o.w = value_pair(sub_zero(codes_to_bf16(w >> 12), z), s, s);
-      *reinterpret_cast<uint4*>(k + (size_t)(t - off) * P.k_stride + hl * 8) = o;
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a = words[4 * i] >> sh, b = words[4 * i + 2] >> sh;
+            p[i] = value_pair(sub_zero(((a & 15u) | ((b & 15u) << 16)) | 0x43004300u, z), s, s);
+          }
+          *reinterpret_cast<uint4*>(P.v + row * P.v_stride + (size_t)g * ISD_HEAD_DIM + hl * 8) = make_uint4(p[0], p[1], p[2], p[3]);
+        }
+      }
     }
-    // V: four dims a lane, all tokens of the run
-    const uint4* src = reinterpret_cast<const uint4*>(tile + kQOffV + lane * 32);
-    const uint4 a = src[0], b = src[1];
-    const uint32_t w[2][4] = {{a.x, a.z, b.x, b.z}, {a.y, a.w, b.y, b.w}};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {  // token pair 2i, 2i + 1
-      const float s0 = bf16_bits_to_f32(meta[32 + 2 * i]), s1 = bf16_bits_to_f32(meta[32 + 2 * i + 1]);
-      const uint32_t z = *reinterpret_cast<const uint32_t*>(meta + 48 + 2 * i);
-      uint32_t p[4];
-#pragma unroll
-      for (int d = 0; d < 4; ++d) p[d] = value_pair(sub_zero(codes_to_bf16(w[i >> 2][d] >> (4 * (i & 3))), z), s0, s1);
-      const int t = 2 * i;
-      if (t >= off && t < off + cnt)
-        *reinterpret_cast<uint2*>(v + (size_t)(t - off) * P.v_stride + lane * 4) =
-            make_uint2(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[2], p[3], 0x5410));
-      if (t + 1 >= off && t + 1 < off + cnt)
-        *reinterpret_cast<uint2*>(v + (size_t)(t + 1 - off) * P.v_stride + lane * 4) =
-            make_uint2(__byte_perm(p[0], p[1], 0x7632), __byte_perm(p[2], p[3], 0x7632));
-    }
-  });
+  }
 }
 
 template <class Kernel>
@@ -229,8 +307,12 @@ int launch_rows(isd_ctx* ctx, const isd_kv_quant_args* a, Kernel kernel, cudaStr
   P.k_stride = (size_t)a->k_row_stride; P.v_stride = (size_t)a->v_row_stride;
   P.slot_map = a->slot_map; P.pool = (uint8_t*)a->kv_pool; P.n_tokens = a->n_tokens;
   P.n_slots = (int64_t)ctx->cfg.num_pages * ISD_PAGE; P.Hkv = ctx->cfg.n_kv_heads; P.global_status = ctx->global_status;
-  const int64_t items = (a->n_tokens + kWindow - 1) / kWindow * P.Hkv;
-  const cudaError_t e = isd_launch_pdl(kernel, dim3((unsigned)((items + kRowsWarps - 1) / kRowsWarps)), dim3(kRowsWarps * 32), 0, stream, P);
+  // all heads in one CTA, where its loop hides the loads' latency, unless that leaves SMs without work
+  const int64_t windows = (a->n_tokens + kWindow - 1) / kWindow;
+  int64_t parts = (int64_t)ctx->num_sms * 8 / windows;
+  parts = parts < 1 ? 1 : (parts > P.Hkv ? P.Hkv : parts);
+  P.heads_each = (int)((P.Hkv + parts - 1) / parts);
+  const cudaError_t e = isd_launch_pdl(kernel, dim3((unsigned)windows, (unsigned)((P.Hkv + P.heads_each - 1) / P.heads_each)), dim3(kRowsThreads), 0, stream, P);
   ctx->launches++;
   return e == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }

@@ -1,5 +1,4 @@
-// The 4-bit KV cache: tile layout, codec and the warp routine that stores a run of tokens (layout and codec are
-// stated in include/isd.h).
+// The 4-bit KV cache: tile layout and codec (stated in include/isd.h).
 #pragma once
 #include "isd_internal.cuh"
 
@@ -88,85 +87,6 @@ __device__ __forceinline__ void unpack8(const uint4& x, float (&f)[8]) {
   f[2] = __uint_as_float(x.y << 16); f[3] = __uint_as_float(x.y & 0xFFFF0000u);
   f[4] = __uint_as_float(x.z << 16); f[5] = __uint_as_float(x.z & 0xFFFF0000u);
   f[6] = __uint_as_float(x.w << 16); f[7] = __uint_as_float(x.w & 0xFFFF0000u);
-}
-
-// nibble mask of the tokens [off, off + cnt) of a page in its V words 0 (tokens 0..7) and 1 (tokens 8..15)
-__device__ __forceinline__ uint32_t token_mask(int off, int cnt, int word) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int t = word * 8 + e;
-    if (t >= off && t < off + cnt) m |= 0xFu << (4 * (e >> 1) + 16 * (e & 1));
-  }
-  return m;
-}
-
-// One warp stores tokens off .. off + cnt - 1 of a page (source rows 0 .. cnt - 1 of k and v, already offset to the kv
-// head) into the page's tile.  Lane = (parity of the token) * 16 + chunk of eight dims, so that a row is read in 16-byte
-// pieces and the even tokens of a V word meet the odd ones in one exchange.  Other warps may be writing other tokens of the
-// same tile (V words hold eight tokens); their nibbles are disjoint, so clearing and setting bits commutes.
-__device__ __forceinline__ void quant_store_run(const __nv_bfloat16* k, size_t k_stride, const __nv_bfloat16* v,
-                                                size_t v_stride, uint8_t* tile, int off, int cnt) {
-  const int lane = threadIdx.x & 31, hl = lane & 15, par = lane >> 4;
-  uint16_t* meta = reinterpret_cast<uint16_t*>(tile + kQOffMeta);
-  uint4 kx[8], vx[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int src = 2 * i + par - off;
-    const bool ok = src >= 0 && src < cnt;
-    kx[i] = ok ? *reinterpret_cast<const uint4*>(k + (size_t)src * k_stride + hl * 8) : make_uint4(0, 0, 0, 0);
-    vx[i] = ok ? *reinterpret_cast<const uint4*>(v + (size_t)src * v_stride + hl * 8) : make_uint4(0, 0, 0, 0);
-  }
-  uint32_t acc[8];  // per dim: this parity's halves of V word 0 (low 16 bits) and word 1 (high 16 bits)
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int t = 2 * i + par;
-    const bool ok = t >= off && t < off + cnt;
-    float f[8];
-    const QuantParam pk = quant_half_warp(kx[i]);
-    unpack8(kx[i], f);
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w |= quant_code(f[e], pk) << (4 * (e >> 1) + 16 * (e & 1));
-    const QuantParam pv = quant_half_warp(vx[i]);
-    unpack8(vx[i], f);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] |= quant_code(f[e], pv) << (4 * (i & 3) + 16 * (i >> 2));
-    if (ok) {
-      *reinterpret_cast<uint32_t*>(tile + (hl >> 2) * 256 + t * 16 + (hl & 3) * 4) = w;
-      if (hl < 4) meta[hl * 16 + t] = hl == 0 ? pk.s_bits : (hl == 1 ? pk.z_bits : (hl == 2 ? pv.s_bits : pv.z_bits));
-    }
-  }
-  // even lanes' half-words are the low halves, odd ones the high halves; each lane ends with four dims
-  uint32_t o[8];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t keep = par ? acc[e + 4] : acc[e], give = par ? acc[e] : acc[e + 4];
-    const uint32_t got = __shfl_xor_sync(0xffffffffu, give, 16);
-    const uint32_t even = par ? got : keep, odd = par ? keep : got;
-    o[2 * e] = __byte_perm(even, odd, 0x5410);
-    o[2 * e + 1] = __byte_perm(even, odd, 0x7632);
-  }
-  uint32_t* dst = reinterpret_cast<uint32_t*>(tile + kQOffV + (hl * 8 + par * 4) * 8);
-  if (cnt == 16) {
-    reinterpret_cast<uint4*>(dst)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    reinterpret_cast<uint4*>(dst)[1] = make_uint4(o[4], o[5], o[6], o[7]);
-  } else {
-    const uint32_t m0 = token_mask(off, cnt, 0), m1 = token_mask(off, cnt, 1);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t m = (e & 1) ? m1 : m0;
-      if (m == 0) continue;
-      if (m != 0xFFFFFFFFu) {
-        atomicAnd(dst + e, ~m);
-        atomicOr(dst + e, o[e] & m);
-      } else {
-        dst[e] = o[e];
-      }
-    }
-  }
 }
 
 }  // namespace
