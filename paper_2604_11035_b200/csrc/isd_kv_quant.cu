@@ -73,21 +73,13 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_quant_kernel(const A
     if (i * 8 >= ql) break;
     const int row = (i * 16 + hw) >> 1;
     const QuantParam p = quant_half_warp(x[i]);
-    float f[8];
-    unpack8(x[i], f);
-    uint32_t c[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = quant_code(f[e], p);
     if (row < ql) {
       const int t = (off0 + row) % ISD_PAGE;
       uint8_t* tile = tile_of((ctx + row) / ISD_PAGE);
       if (hw & 1) {
-        codes[row][hl] = make_uint2(c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24), c[4] | (c[5] << 8) | (c[6] << 16) | (c[7] << 24));
+        codes[row][hl] = quant_bytes(x[i], p);
       } else {
-        uint32_t w = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w |= c[e] << (4 * (e >> 1) + 16 * (e & 1));
-        *reinterpret_cast<uint32_t*>(tile + (hl >> 2) * 256 + t * 16 + (hl & 3) * 4) = w;
+        *reinterpret_cast<uint32_t*>(tile + (hl >> 2) * 256 + t * 16 + (hl & 3) * 4) = quant_word(x[i], p);
       }
       if (hl < 2) reinterpret_cast<uint16_t*>(tile + kQOffMeta)[((hw & 1) * 2 + hl) * 16 + t] = hl == 0 ? p.s_bits : p.z_bits;
     }
@@ -196,41 +188,39 @@ __global__ void __launch_bounds__(kRowsThreads) kv_write_quant_kernel(const Rows
         vn = *reinterpret_cast<const uint4*>(v + (size_t)(g + 1) * ISD_HEAD_DIM);
       }
       const QuantParam pk = quant_half_warp(kx), pv = quant_half_warp(vx);
-      float f[8];
-      unpack8(kx, f);
-      uint32_t w = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w |= quant_code(f[e], pk) << (4 * (e >> 1) + 16 * (e & 1));
-      unpack8(vx, f);
-      uint32_t c[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = quant_code(f[e], pv);
+      const uint32_t w = quant_word(kx, pk);
       if (mine) {
         *reinterpret_cast<uint32_t*>(tile + (hl >> 2) * 256 + hw * 16 + (hl & 3) * 4) = w;
         if (hl < 4)
           reinterpret_cast<uint16_t*>(tile + kQOffMeta)[hl * 16 + hw] = hl == 0 ? pk.s_bits : (hl == 1 ? pk.z_bits : (hl == 2 ? pv.s_bits : pv.z_bits));
       }
-      codes[buf][hw][hl] = make_uint2(c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24), c[4] | (c[5] << 8) | (c[6] << 16) | (c[7] << 24));
+      codes[buf][hw][hl] = quant_bytes(vx, pv);
       __syncthreads();
-      {  // thread = (dim, half of the page)
-        const int dim = threadIdx.x >> 1, half = threadIdx.x & 1;
-        const uint8_t* bytes = reinterpret_cast<const uint8_t*>(codes[buf]);
-        uint32_t word = 0, mask = 0;
+      // V words: thread = (four dims, half of the page), two warps of the eight by turns
+      if (((threadIdx.x >> 6) & 3) == (g & 3)) {
+        const int quad = (threadIdx.x & 63) >> 1, half = threadIdx.x & 1;
+        const uint32_t* bytes = reinterpret_cast<const uint32_t*>(codes[buf]) + quad;  // [token][32 words]
+        uint32_t b[8], word[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int tok = half * 8 + e, sh = 4 * (e >> 1) + 16 * (e & 1);
-          if (tok >= off && tok < off + cnt) {
-            word |= (uint32_t)bytes[tok * ISD_HEAD_DIM + dim] << sh;
-            mask |= 0xFu << sh;
-          }
+        for (int e = 0; e < 8; ++e) b[e] = bytes[(half * 8 + e) * 32];
+        v_words(b, word);
+        uint32_t* dst = reinterpret_cast<uint32_t*>(tile + kQOffV) + quad * 8 + half;
+        uint32_t mask = 0xFFFFFFFFu;
+        if (cnt < 16) {
+          mask = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (half * 8 + e >= off && half * 8 + e < off + cnt) mask |= 0xFu << (4 * (e >> 1) + 16 * (e & 1));
         }
-        uint32_t* dst = reinterpret_cast<uint32_t*>(tile + kQOffV) + threadIdx.x;
-        if (mask == 0xFFFFFFFFu) {
-          *dst = word;
-        } else if (mask) {
-          // other CTAs may be writing other tokens of the word; their nibbles are disjoint, so clearing and setting bits commutes
-          atomicAnd(dst, ~mask);
-          atomicOr(dst, word);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (mask == 0xFFFFFFFFu) {
+            dst[2 * i] = word[i];
+          } else if (mask) {
+            // other CTAs may be writing other tokens of the word; their nibbles are disjoint, so clearing and setting bits commutes
+            atomicAnd(dst + 2 * i, ~mask);
+            atomicOr(dst + 2 * i, word[i] & mask);
+          }
         }
       }
       kx = kn;
@@ -246,55 +236,57 @@ __device__ __forceinline__ uint32_t value_pair(uint32_t d, float s0, float s1) {
 }
 
 // The way back: the tile of a (page, head) comes into shared memory whole (two buffers; the next head's is under way), then a
-// half-warp writes its token's rows in 16-byte pieces.  Bound: HBM (136 bytes in, 512 out per token and head).
+// half-warp writes its token's K row and a warp two tokens' V rows.  Bound: HBM (136 bytes in, 512 out per token and head).
 __global__ void __launch_bounds__(kRowsThreads) kv_read_quant_kernel(const RowsParams P) {
   constexpr int kVecs = kQTile / 16;  // 136
-  __shared__ uint4 tiles[2][kVecs];
+  __shared__ uint4 tiles[2][kVecs + 4];  // K's four chunks of 16 vectors a vector further apart, for the banks' sake
   pdl_wait();
   pdl_launch_dependents();
-  const int hw = threadIdx.x >> 4, hl = threadIdx.x & 15;
+  const int hw = threadIdx.x >> 4, hl = threadIdx.x & 15, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g0 = blockIdx.y * P.heads_each, g1 = min(g0 + P.heads_each, P.Hkv);
+  const bool loads = threadIdx.x < kVecs;
+  const int at = threadIdx.x < 64 ? threadIdx.x + (threadIdx.x >> 4) : threadIdx.x + 4;
   Runs runs;
   runs.find(P, (int64_t)blockIdx.x * kWindow, g0 == 0 && threadIdx.x < 32);
   int64_t t, page;
   int off, cnt, buf = 0;
   while (runs.next(t, off, cnt, page)) {
-    const bool mine = hw >= off && hw < off + cnt, loads = threadIdx.x < kVecs;
     const uint4* src = reinterpret_cast<const uint4*>(P.pool + (size_t)page * P.Hkv * kQTile) + threadIdx.x;
-    const size_t row = (size_t)(t + (mine ? hw - off : 0));
     uint4 x = make_uint4(0, 0, 0, 0);
     if (loads) x = src[(size_t)g0 * kVecs];
     for (int g = g0; g < g1; ++g, buf ^= 1) {
-      if (loads) tiles[buf][threadIdx.x] = x;
+      if (loads) tiles[buf][at] = x;
       __syncthreads();
       if (loads && g + 1 < g1) x = src[(size_t)(g + 1) * kVecs];
-      if (mine) {
-        const uint8_t* tile = reinterpret_cast<const uint8_t*>(tiles[buf]);
-        const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + kQOffMeta);
-        {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + (hl >> 2) * 256 + hw * 16 + (hl & 3) * 4);
-          const float s = bf16_bits_to_f32(meta[hw]);
-          const uint32_t z = meta[16 + hw] * 0x10001u;
-          uint4 o;
-          o.x = value_pair(sub_zero(codes_to_bf16(w), z), s, s);
-          o.y = value_pair(sub_zero(codes_to_bf16(w >> 4), z), s, s);
-          o.z = value_pair(sub_zero(codes_to_bf16(w >> 8), z), s, s);
-          o.w = value_pair(sub_zero(codes_to_bf16(w >> 12), z), s, s);
-          *reinterpret_cast<uint4*>(P.k + row * P.k_stride + (size_t)g * ISD_HEAD_DIM + hl * 8) = o;
-        }
-        {
-          const float s = bf16_bits_to_f32(meta[32 + hw]);
-          const uint32_t z = meta[48 + hw] * 0x10001u;
-          const int sh = 4 * ((hw & 7) >> 1) + 16 * (hw & 1);
-          const uint32_t* words = reinterpret_cast<const uint32_t*>(tile + kQOffV) + hl * 16 + (hw >> 3);  // [dim][2]
-          uint32_t p[4];
+      const uint8_t* tile = reinterpret_cast<const uint8_t*>(tiles[buf]) + 64;  // V codes and scales
+      const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + kQOffMeta);
+      if (hw >= off && hw < off + cnt) {  // K: half-warp per token, eight dims a lane
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(tile - 64 + (hl >> 2) * 272 + hw * 16 + (hl & 3) * 4);
+        const float s = bf16_bits_to_f32(meta[hw]);
+        const uint32_t z = meta[16 + hw] * 0x10001u;
+        uint4 o;
+        o.x = value_pair(sub_zero(codes_to_bf16(w), z), s, s);
+        o.y = value_pair(sub_zero(codes_to_bf16(w >> 4), z), s, s);
+        o.z = value_pair(sub_zero(codes_to_bf16(w >> 8), z), s, s);
+        o.w = value_pair(sub_zero(codes_to_bf16(w >> 12), z), s, s);
+        *reinterpret_cast<uint4*>(P.k + (size_t)(t + hw - off) * P.k_stride + (size_t)g * ISD_HEAD_DIM + hl * 8) = o;
+      }
+      const int tok = 2 * warp;  // V: warp per pair of tokens, four dims a lane
+      if (tok + 1 >= off && tok < off + cnt) {
+        const uint4* words = reinterpret_cast<const uint4*>(tile + kQOffV + lane * 32);  // [four dims][2]
+        const uint4 a = words[0], b = words[1];
+        const bool hi = warp >= 4;
+        const int sh = 4 * (warp & 3);
+        const uint32_t w[4] = {hi ? a.y : a.x, hi ? a.w : a.z, hi ? b.y : b.x, hi ? b.w : b.z};
+        const float s0 = bf16_bits_to_f32(meta[32 + tok]), s1 = bf16_bits_to_f32(meta[33 + tok]);
+        const uint32_t z = *reinterpret_cast<const uint32_t*>(meta + 48 + tok);
+        uint32_t p[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t a = words[4 * i] >> sh, b = words[4 * i + 2] >> sh;
-            p[i] = value_pair(sub_zero(((a & 15u) | ((b & 15u) << 16)) | 0x43004300u, z), s, s);
-          }
-          *reinterpret_cast<uint4*>(P.v + row * P.v_stride + (size_t)g * ISD_HEAD_DIM + hl * 8) = make_uint4(p[0], p[1], p[2], p[3]);
-        }
+        for (int i = 0; i < 4; ++i) p[i] = value_pair(sub_zero(codes_to_bf16(w[i] >> sh), z), s0, s1);
+        __nv_bfloat16* v = P.v + (size_t)(t + tok - off) * P.v_stride + (size_t)g * ISD_HEAD_DIM + lane * 4;
+        if (tok >= off) *reinterpret_cast<uint2*>(v) = make_uint2(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[2], p[3], 0x5410));
+        if (tok + 1 < off + cnt)
+          *reinterpret_cast<uint2*>(v + P.v_stride) = make_uint2(__byte_perm(p[0], p[1], 0x7632), __byte_perm(p[2], p[3], 0x7632));
       }
     }
   }

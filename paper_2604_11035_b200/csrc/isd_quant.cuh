@@ -25,42 +25,94 @@ __device__ __forceinline__ uint32_t sub_zero(uint32_t c128, uint32_t z128) {
 
 // Parameters of one vector's codec.
 struct QuantParam {
-  float s, inv;    // scale, correctly rounded reciprocal
+  float s, inv;       // scale, reciprocal to an ulp or two
   int z;
-  bool live;       // s > 0 and finite
-  bool plain_div;  // scale too small or too large for the reciprocal form below
+  bool live;          // s > 0 and finite
+  bool plain_div;     // scale too small or too large for the division steps below
   uint16_t s_bits, z_bits;
 };
 
+// Quotients of the codec.  x / s has to be rounded as its correctly rounded 32-bit quotient rounds, that is, a tie x / s = k + 1/2
+// goes to the even side: q0 = x * (1 / s) is off by an ulp or two, and one step with the exact remainder leaves an error of 2^-45
+// of it, so that a tie comes out as one; x and s have 8-bit significands, so a quotient that is not a tie is at least 2^-14
+// of itself away from one.
+__device__ __forceinline__ float quant_div(float x, float s, float inv) {
+  const float q0 = x * inv;
+  return fmaf(fmaf(-q0, s, x), inv, q0);
+}
+
 __device__ __forceinline__ QuantParam quant_param(float lo, float hi) {
   QuantParam p;
-  const float t = __fdiv_rn(hi - lo, 15.f);
-  const __nv_bfloat16 sb = __float2bfloat16_rn(t);
-  p.s = __bfloat162float(sb);
-  const bool bad = !(p.s <= 3.3895e38f);  // NaN or infinite
-  p.live = !bad && p.s > 0.f;
-  p.plain_div = !(p.s > 1e-30f && p.s < 1e30f);
-  p.inv = p.live && !p.plain_div ? __frcp_rn(p.s) : 0.f;
-  p.z = p.live ? (int)fminf(fmaxf(rintf(__fdiv_rn(-lo, p.s)), 0.f), 15.f) : 0;
-  p.s_bits = bad ? (uint16_t)0x7FC0 : __bfloat16_as_ushort(sb);
+  const float range = hi - lo;
+  if (range > 1e-28f && range < 1e28f) {
+    // (the same step gives range / 15 correctly rounded for all significands: checked one by one)
+    const __nv_bfloat16 sb = __float2bfloat16_rn(quant_div(range, 15.f, 1.f / 15.f));
+    p.s = __bfloat162float(sb);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(p.s));
+    p.inv = fmaf(fmaf(-p.s, r, 1.f), r, r);
+    p.z = (int)fminf(rintf(quant_div(-lo, p.s, p.inv)), 15.f);  // (-lo >= 0)
+    p.live = true;
+    p.plain_div = false;
+    p.s_bits = __bfloat16_as_ushort(sb);
+  } else {  // NaN, infinite, zero, or near the ends of the exponents
+    const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(range, 15.f));
+    p.s = __bfloat162float(sb);
+    const bool bad = !(p.s <= 3.3895e38f);
+    p.live = !bad && p.s > 0.f;
+    p.plain_div = true;
+    p.inv = 0.f;
+    p.z = p.live ? (int)fminf(fmaxf(rintf(__fdiv_rn(-lo, p.s)), 0.f), 15.f) : 0;
+    p.s_bits = bad ? (uint16_t)0x7FC0 : __bfloat16_as_ushort(sb);
+  }
   p.z_bits = (uint16_t)(kQZeroOne + p.z);
   return p;
 }
 
-// clamp(round(x / s) + z, 0, 15).  The quotient has to be the correctly rounded one (a tie x / s = k + 1/2 goes to the
-// even side): q0 = x * (1/s) is off by an ulp or two, and one correction with the exact remainder rounds it correctly
-// (the usual division step for a correctly rounded reciprocal; x and s have 8-bit significands, so a quotient that is
-// not a tie is at least 2^-14 of itself away from one).  round() adds 1.5 * 2^23, where a float's unit is 1.
-__device__ __forceinline__ uint32_t quant_code(float x, const QuantParam& p) {
-  float q;
+// Eight codes clamp(round(x / s) + z, 0, 15), the i-th at bit shift(i) of the 64-bit result.  round() adds 1.5 * 2^23, where a
+// float's unit is 1; the clamp is taken there (bounds 1.5 * 2^23 - z and 15 more), and the codes, offset by the same
+// constant, are summed at their places and freed of it all at once.
+template <class Shift>
+__device__ __forceinline__ uint2 quant_codes(const uint4& x, const QuantParam& p, Shift shift) {
+  float f[8] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u),
+                __uint_as_float(x.z << 16), __uint_as_float(x.z & 0xFFFF0000u), __uint_as_float(x.w << 16), __uint_as_float(x.w & 0xFFFF0000u)};
+  const uint32_t zero = 0x4B400000u - (uint32_t)p.z;  // bits of 1.5 * 2^23 - z
+  uint32_t out[2] = {0u, 0u};
   if (p.plain_div) {
-    q = p.live ? __fdiv_rn(x, p.s) : 0.f;
-  } else {
-    const float q0 = x * p.inv;
-    q = fmaf(fmaf(-q0, p.s, x), p.inv, q0);
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      const float v = i == 0 ? f[0] : i == 1 ? f[1] : i == 2 ? f[2] : i == 3 ? f[3] : i == 4 ? f[4] : i == 5 ? f[5] : i == 6 ? f[6] : f[7];
+      const float q = p.live ? __fdiv_rn(v, p.s) : 0.f;
+      const int c = min(max(__float_as_int(q + 12582912.f) - 0x4B400000 + p.z, 0), 15);
+      const uint32_t at = (uint32_t)c << (shift(i) & 31);
+      if (shift(i) < 32) out[0] |= at; else out[1] |= at;
+    }
+    return make_uint2(out[0], out[1]);
   }
-  const int c = __float_as_int(q + 12582912.f) - 0x4B400000 + p.z;
-  return (uint32_t)min(max(c, 0), 15);
+  const float least = __uint_as_float(zero), most = __uint_as_float(zero + 15u);
+  const uint64_t s2 = pack2(-p.s, -p.s), i2 = pack2(p.inv, p.inv), m2 = pack2(12582912.f, 12582912.f);
+  uint32_t places[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const uint64_t v = pack2(f[i], f[i + 1]), q0 = mul2(v, i2);
+    float a, b;
+    unpack2(add2(fma2(fma2(q0, s2, v), i2, q0), m2), a, b);
+    a = fminf(fmaxf(a, least), most);
+    b = fminf(fmaxf(b, least), most);
+    out[shift(i) >> 5] += __float_as_uint(a) << (shift(i) & 31);
+    out[shift(i + 1) >> 5] += __float_as_uint(b) << (shift(i + 1) & 31);
+    places[shift(i) >> 5] += 1u << (shift(i) & 31);
+    places[shift(i + 1) >> 5] += 1u << (shift(i + 1) & 31);
+  }
+  return make_uint2(out[0] - zero * places[0], out[1] - zero * places[1]);
+}
+// a word of the cache: element i at bit 4 (i / 2) + 16 (i % 2)
+__device__ __forceinline__ uint32_t quant_word(const uint4& x, const QuantParam& p) {
+  return quant_codes(x, p, [](int i) { return 4 * (i >> 1) + 16 * (i & 1); }).x;
+}
+// a byte a code
+__device__ __forceinline__ uint2 quant_bytes(const uint4& x, const QuantParam& p) {
+  return quant_codes(x, p, [](int i) { return 8 * i; });
 }
 
 __device__ __forceinline__ uint32_t hmin2_nan(uint32_t a, uint32_t b) { return as_u32(__hmin2_nan(as_bf162(a), as_bf162(b))); }
@@ -82,11 +134,15 @@ __device__ __forceinline__ QuantParam quant_half_warp(const uint4& x) {
   return quant_param(__uint_as_float(zz << 16), __uint_as_float(ww & 0xFFFF0000u));
 }
 
-__device__ __forceinline__ void unpack8(const uint4& x, float (&f)[8]) {
-  f[0] = __uint_as_float(x.x << 16); f[1] = __uint_as_float(x.x & 0xFFFF0000u);
-  f[2] = __uint_as_float(x.y << 16); f[3] = __uint_as_float(x.y & 0xFFFF0000u);
-  f[4] = __uint_as_float(x.z << 16); f[5] = __uint_as_float(x.z & 0xFFFF0000u);
-  f[6] = __uint_as_float(x.w << 16); f[7] = __uint_as_float(x.w & 0xFFFF0000u);
+// The V words of four dims for eight tokens, whose codes for these dims are bytes of w[0..7]: a byte takes the codes of tokens
+// 4 apart in the word's order (0 and 2, 4 and 6, 1 and 3, 5 and 7), then the 4 x 4 bytes are transposed.
+__device__ __forceinline__ void v_words(const uint32_t (&w)[8], uint32_t (&out)[4]) {
+  const uint32_t a = w[0] + (w[2] << 4), b = w[4] + (w[6] << 4), c = w[1] + (w[3] << 4), d = w[5] + (w[7] << 4);
+  const uint32_t ab0 = __byte_perm(a, b, 0x5140), ab1 = __byte_perm(a, b, 0x7362), cd0 = __byte_perm(c, d, 0x5140), cd1 = __byte_perm(c, d, 0x7362);
+  out[0] = __byte_perm(ab0, cd0, 0x5410);
+  out[1] = __byte_perm(ab0, cd0, 0x7632);
+  out[2] = __byte_perm(ab1, cd1, 0x5410);
+  out[3] = __byte_perm(ab1, cd1, 0x7632);
 }
 
 }  // namespace
