@@ -159,42 +159,44 @@ struct Runs {
   }
 };
 
-// A CTA walks the runs of a window and, for each, some of the kv heads: half-warp = token of the page, lane = eight dims.  K
-// words are complete in a lane; V words hold eight tokens of a dim and are put together through shared memory (two buffers:
-// one barrier a head).  The next head's rows are fetched before this one is encoded.
-// Bound: HBM (512 bytes in, 136 out per token and head).  As one warp per (run, head), which encoded its 16 tokens one after the
-// other, the write took twice as long.
+// A CTA walks the runs of a window and, for each, some of the kv heads: warps 0-3 take K, warps 4-7 V, a quarter-warp per
+// token, 16 dims a lane in two pieces (8 lanes share the cost of a vector's parameters, which is as large as that of its
+// codes).  K words are complete in a lane; V words hold eight tokens of a dim and are put together through shared memory (two
+// buffers: one barrier a head).  The next head's rows are fetched before this one is encoded.
+// Bound: instruction issue (HBM: 512 bytes in, 136 out per token and head).
 __global__ void __launch_bounds__(kRowsThreads) kv_write_quant_kernel(const RowsParams P) {
   __shared__ uint2 codes[2][16][16];  // V codes, a byte each: [buffer][token][eight dims]
   pdl_wait();
   pdl_launch_dependents();
-  const int hw = threadIdx.x >> 4, hl = threadIdx.x & 15;
+  const bool is_v = threadIdx.x >= 128;
+  const int tok = (threadIdx.x & 127) >> 3, hl = threadIdx.x & 7;
   const int g0 = blockIdx.y * P.heads_each, g1 = min(g0 + P.heads_each, P.Hkv);
   Runs runs;
   runs.find(P, (int64_t)blockIdx.x * kWindow, g0 == 0 && threadIdx.x < 32);
   int64_t t, page;
   int off, cnt, buf = 0;
   while (runs.next(t, off, cnt, page)) {
-    const bool mine = hw >= off && hw < off + cnt;
-    const size_t row = (size_t)(t + (mine ? hw - off : 0));
-    const __nv_bfloat16* k = P.k + row * P.k_stride + hl * 8;
-    const __nv_bfloat16* v = P.v + row * P.v_stride + hl * 8;
-    uint4 kx = *reinterpret_cast<const uint4*>(k + (size_t)g0 * ISD_HEAD_DIM), vx = *reinterpret_cast<const uint4*>(v + (size_t)g0 * ISD_HEAD_DIM);
+    const bool mine = tok >= off && tok < off + cnt;
+    const size_t row = (size_t)(t + (mine ? tok - off : 0));
+    const uint4* src = reinterpret_cast<const uint4*>(is_v ? P.v + row * P.v_stride : P.k + row * P.k_stride) + hl;
+    uint4 x = src[g0 * 16], y = src[g0 * 16 + 8];  // dims 8 hl .. and 64 + 8 hl ..
     for (int g = g0; g < g1; ++g, buf ^= 1) {
       uint8_t* tile = P.pool + ((size_t)page * P.Hkv + g) * kQTile;
-      uint4 kn = kx, vn = vx;
+      uint4 xn = x, yn = y;
       if (g + 1 < g1) {
-        kn = *reinterpret_cast<const uint4*>(k + (size_t)(g + 1) * ISD_HEAD_DIM);
-        vn = *reinterpret_cast<const uint4*>(v + (size_t)(g + 1) * ISD_HEAD_DIM);
+        xn = src[(g + 1) * 16];
+        yn = src[(g + 1) * 16 + 8];
       }
-      const QuantParam pk = quant_half_warp(kx), pv = quant_half_warp(vx);
-      const uint32_t w = quant_word(kx, pk);
-      if (mine) {
-        *reinterpret_cast<uint32_t*>(tile + (hl >> 2) * 256 + hw * 16 + (hl & 3) * 4) = w;
-        if (hl < 4)
-          reinterpret_cast<uint16_t*>(tile + kQOffMeta)[hl * 16 + hw] = hl == 0 ? pk.s_bits : (hl == 1 ? pk.z_bits : (hl == 2 ? pv.s_bits : pv.z_bits));
+      const QuantParam p = quant_quarter_warp(x, y);
+      if (mine && hl < 2) reinterpret_cast<uint16_t*>(tile + kQOffMeta)[((is_v ? 2 : 0) + hl) * 16 + tok] = hl == 0 ? p.s_bits : p.z_bits;
+      if (is_v) {
+        codes[buf][tok][hl] = quant_bytes(x, p);
+        codes[buf][tok][8 + hl] = quant_bytes(y, p);
+      } else if (mine) {
+        uint32_t* dst = reinterpret_cast<uint32_t*>(tile) + (hl >> 2) * 64 + tok * 4 + (hl & 3);
+        dst[0] = quant_word(x, p);
+        dst[128] = quant_word(y, p);
       }
-      codes[buf][hw][hl] = quant_bytes(vx, pv);
       __syncthreads();
       // V words: thread = (four dims, half of the page), two warps of the eight by turns
       if (((threadIdx.x >> 6) & 3) == (g & 3)) {
@@ -223,8 +225,8 @@ __global__ void __launch_bounds__(kRowsThreads) kv_write_quant_kernel(const Rows
           }
         }
       }
-      kx = kn;
-      vx = vn;
+      x = xn;
+      y = yn;
     }
   }
 }

@@ -118,20 +118,28 @@ __device__ __forceinline__ uint2 quant_bytes(const uint4& x, const QuantParam& p
 __device__ __forceinline__ uint32_t hmin2_nan(uint32_t a, uint32_t b) { return as_u32(__hmin2_nan(as_bf162(a), as_bf162(b))); }
 __device__ __forceinline__ uint32_t hmax2_nan(uint32_t a, uint32_t b) { return as_u32(__hmax2_nan(as_bf162(a), as_bf162(b))); }
 
-// Codec parameters of the 128 values whose 16 lanes of a half-warp hold eight each (NaN propagates).
-__device__ __forceinline__ QuantParam quant_half_warp(const uint4& x) {
-  uint32_t mn = hmin2_nan(hmin2_nan(x.x, x.y), hmin2_nan(x.z, x.w));
-  uint32_t mx = hmax2_nan(hmax2_nan(x.x, x.y), hmax2_nan(x.z, x.w));
+// Codec parameters of the 128 values that LANES neighbouring lanes hold between them (NaN propagates); mn, mx: the lane's
+// minima and maxima, in pairs.
+template <int LANES>
+__device__ __forceinline__ QuantParam quant_lanes(uint32_t mn, uint32_t mx) {
   // low half: minimum, high half: maximum
   const uint32_t a = __byte_perm(mn, mx, 0x5410), b = __byte_perm(mn, mx, 0x7632);
   uint32_t m = __byte_perm(hmin2_nan(a, b), hmax2_nan(a, b), 0x7610);
 #pragma unroll
-  for (int off = 1; off < 16; off <<= 1) {
+  for (int off = 1; off < LANES; off <<= 1) {
     const uint32_t o = __shfl_xor_sync(0xffffffffu, m, off);
     m = __byte_perm(hmin2_nan(m, o), hmax2_nan(m, o), 0x7610);
   }
   const uint32_t zz = as_u32(__hmin2_nan(as_bf162(m), as_bf162(0u))), ww = as_u32(__hmax2_nan(as_bf162(m), as_bf162(0u)));
   return quant_param(__uint_as_float(zz << 16), __uint_as_float(ww & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint32_t hmin2_nan(const uint4& x) { return hmin2_nan(hmin2_nan(x.x, x.y), hmin2_nan(x.z, x.w)); }
+__device__ __forceinline__ uint32_t hmax2_nan(const uint4& x) { return hmax2_nan(hmax2_nan(x.x, x.y), hmax2_nan(x.z, x.w)); }
+// eight values a lane, 16 lanes
+__device__ __forceinline__ QuantParam quant_half_warp(const uint4& x) { return quant_lanes<16>(hmin2_nan(x), hmax2_nan(x)); }
+// sixteen values a lane, 8 lanes
+__device__ __forceinline__ QuantParam quant_quarter_warp(const uint4& x, const uint4& y) {
+  return quant_lanes<8>(hmin2_nan(hmin2_nan(x), hmin2_nan(y)), hmax2_nan(hmax2_nan(x), hmax2_nan(y)));
 }
 
 // The V words of four dims for eight tokens, whose codes for these dims are bytes of w[0..7]: a byte takes the codes of tokens
