@@ -31,13 +31,11 @@
 
 namespace {
 
-constexpr int kQuantThreads = 640;
 constexpr int kStageQ = 8 * kQTile;    // one tile of 128 keys: eight pages' tiles
 constexpr int kQuantSegCost = 4;       // fixed cost of a segment in units of one tile's time
 constexpr float kNoRef = 3.0e38f;      // any score plus this asks for a reference; a masked one (-inf) does not
 constexpr int kScaleBufs = 4;          // the decoders run at most three tiles ahead of the softmax
 constexpr int kSegRing = 4;
-constexpr int kSegReaders = 19;        // warps
 
 struct QuantParams : SplitParams {
   int max_pages, num_pages;
@@ -49,22 +47,26 @@ struct QuantParams : SplitParams {
   unsigned long long wait_ns;
 };
 
-// Sizes that depend on the most rows a block of this context can have (64 or 128).
+// Sizes that depend on the most rows a block of this context can have (32, 64 or 128).
 template <int RMAX>
 struct Cfg {
-  static constexpr int kStages = RMAX == 64 ? 8 : 4;
-  static constexpr int kA = RMAX == 64 ? 2 : 1;       // buffers of the decoded K and V tiles (64 columns each)
-  static constexpr int kChunks = RMAX / 32;           // chunks of 16 rows of a softmax warpgroup, at most
+  static constexpr int kStages = RMAX <= 64 ? 8 : 4;
+  static constexpr int kA = RMAX <= 64 ? 2 : 1;       // buffers of the decoded K and V tiles (64 columns each)
+  static constexpr int kGroups = RMAX == 32 ? 2 : 4;  // softmax warpgroups, which share the rows
+  static constexpr int kChunks = RMAX / 16 / kGroups; // chunks of 16 rows of a softmax warpgroup, at most (1 or 2)
   static constexpr int kCols = kChunks * 16;
+  static constexpr int kSoftmaxEnd = 8 + 4 * kGroups; // warps: 8 decode, then softmax, then copies, QK, PV, segments and Q
+  static constexpr int kThreads = (kSoftmaxEnd + 4) * 32;
+  static constexpr int kSegReaders = kSoftmaxEnd + 3;
   static constexpr int kSmQ = 0;                      // [2 segments][2 halves of d][RMAX rows][128 B], 128-byte swizzle
-  static constexpr int kSmP = kSmQ + 2 * RMAX * 256;  // [2 tiles][RMAX / 64 halves of rows][128 keys][128 B], 128-byte swizzle
-  static constexpr int kPBytes = RMAX / 64 * 16384;
+  static constexpr int kSmP = kSmQ + 2 * RMAX * 256;  // [2 tiles][halves of 64 rows][128 keys][128 B], 128-byte swizzle
+  static constexpr int kPBytes = (RMAX + 63) / 64 * 16384;
   static constexpr int kSmRing = kSmP + 2 * kPBytes;
   static constexpr int kSmBar = kSmRing + kStages * kStageQ;
   static constexpr int kSmScale = kSmBar + 512;       // [kScaleBufs][128] x {sk * scale2, sv}
-  static constexpr int kSmNegM = kSmScale + kScaleBufs * 128 * 8;  // [2 warpgroups][64] -reference maximum per row (kNoRef: none yet)
-  static constexpr int kSmF = kSmNegM + 512;          // [2 warpgroups][64] factor of a raise, of the epilogue
-  static constexpr int kSmRed = kSmF + 512;           // [2 warpgroups][4 warps][64] warp results
+  static constexpr int kSmNegM = kSmScale + kScaleBufs * 128 * 8;  // [warpgroup][32] -reference maximum per row (kNoRef: none yet)
+  static constexpr int kSmF = kSmNegM + 512;          // [warpgroup][32] factor of a raise, of the epilogue
+  static constexpr int kSmRed = kSmF + 512;           // [warpgroup][4 warps][32] warp results
   static constexpr int kSmSeg = kSmRed + 2048;         // ring of segments, 32 bytes each
   static constexpr int kSmPrefix = kSmSeg + 128;
   static constexpr int kSmSlot = kSmPrefix + (kMaxSmemPrefixSlots + 1) * 4 + 12;
@@ -80,9 +82,10 @@ struct Cfg {
     QFULL = ODONE + 2, QFREE = QFULL + 2, OFREE = QFREE + 2, SEGFULL, SEGFREE = SEGFULL + 4, COUNT = SEGFREE + 4
   };
   static_assert(COUNT * 8 + 32 <= 512, "barrier block");
-  // Registers a thread: 640 threads are launched with 96 each and share them out anew.
-  static constexpr int kRegsSoftmax = RMAX == 64 ? 136 : 144, kRegsDecode = 72, kRegsRest = RMAX == 64 ? 64 : 48;
-  static_assert(2 * 128 * kRegsSoftmax + 2 * 128 * kRegsDecode + 128 * kRegsRest <= kQuantThreads * 96, "register split");
+  // Registers a thread: shared out anew from what the threads are launched with (96 or 72 each).
+  static constexpr int kRegsLaunch = kThreads == 640 ? 96 : 72;
+  static constexpr int kRegsSoftmax = kThreads == 640 ? 112 : 80, kRegsDecode = kThreads == 640 ? 88 : 64, kRegsRest = kThreads == 640 ? 80 : 56;
+  static_assert(128 * (kGroups * kRegsSoftmax + 2 * kRegsDecode + kRegsRest) <= kThreads * kRegsLaunch, "register split");
 };
 
 // 16 columns of the thread's lane, arrived (load and wait in one statement: what uses the registers cannot be moved between)
@@ -142,15 +145,10 @@ __device__ __forceinline__ bool mbar_try_wait_long(uint32_t bar, uint32_t parity
   return ok != 0;
 }
 
-// one look at a phase; a try_wait that finds its phase complete still costs 150 cycles with a suspension limit
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n.reg .pred p;\n"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-      "selp.u32 %0, 1, 0, p;\n}"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
+// Arrival of lane 0 without a branch around it (a dozen arrivals a tile: their branches cost the softmax warps more than the
+// arrivals)
+__device__ __forceinline__ void arrive_lane0(uint32_t bar, int lane) {
+  asm volatile("{\n.reg .pred p;\nsetp.eq.s32 p, %1, 0;\n@p mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(bar), "r"(lane) : "memory");
 }
 
 struct Shared {  // what every role needs
@@ -159,7 +157,7 @@ struct Shared {  // what every role needs
   volatile int* abort_flag;
   __device__ __forceinline__ uint32_t bar(uint32_t i) const { return bar0 + 8u * i; }
   __device__ __forceinline__ bool wait(uint32_t i, uint32_t parity) const {
-    if (mbar_test(bar(i), parity & 1u)) return true;
+    if (mbar_try_wait_long(bar(i), parity & 1u)) return true;
     unsigned long long t0 = 0;  // (at most one more suspension after another thread has given up)
     while (!mbar_try_wait_long(bar(i), parity & 1u)) {
       const unsigned long long now = isd_now_ns();
@@ -203,21 +201,21 @@ __device__ __forceinline__ bool give_segment(const Shared& S, uint32_t k, const 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Softmax and epilogue of one segment by warpgroup wg (0, 1), which has half of the block's chunks of 16 rows
+// Softmax and epilogue of one segment by warpgroup wg, which has its share of the block's chunks of 16 rows
 // ------------------------------------------------------------------------------------------------
 template <int RMAX>
 __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Segment& sg, const Shared& S, int wg, uint32_t& n) {
   using C = Cfg<RMAX>;
-  constexpr bool kKeep = C::kChunks <= 2;  // arguments stay in registers between the vote and the exponentials
+  constexpr bool kKeep = C::kChunks == 1;  // arguments stay in registers between the vote and the exponentials
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, tl = warp * 32 + lane;  // tl: TMEM lane = key of the tile = dim of O
   const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
   const int rows = sg.q_len * P.G, chunks = (rows + 15) >> 4;
-  const int c0 = wg == 0 ? 0 : (chunks + 1) >> 1, mine = wg == 0 ? (chunks + 1) >> 1 : chunks >> 1;
+  const int each = (chunks + C::kGroups - 1) / C::kGroups, c0 = min(wg * each, chunks), mine = min(each, chunks - c0);
   const int cnt = sg.j1 - sg.j0;
-  float* neg_m = reinterpret_cast<float*>(S.smem + C::kSmNegM) + wg * 64;
-  float* fac = reinterpret_cast<float*>(S.smem + C::kSmF) + wg * 64;
-  float* red = reinterpret_cast<float*>(S.smem + C::kSmRed) + wg * 256;  // [warp][64]
-  const uint32_t neg_m_a = S.base + C::kSmNegM + wg * 256, fac_a = S.base + C::kSmF + wg * 256;
+  float* neg_m = reinterpret_cast<float*>(S.smem + C::kSmNegM) + wg * 32;
+  float* fac = reinterpret_cast<float*>(S.smem + C::kSmF) + wg * 32;
+  float* red = reinterpret_cast<float*>(S.smem + C::kSmRed) + wg * 128;  // [warp][32]
+  const uint32_t neg_m_a = S.base + C::kSmNegM + wg * 128, fac_a = S.base + C::kSmF + wg * 128;
   uint64_t l2[C::kChunks * 8];  // row sums of this lane's keys, pairs of rows
 #pragma unroll
   for (int i = 0; i < C::kChunks * 8; ++i) l2[i] = 0;
@@ -290,13 +288,13 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
             const float s = warp_max(__uint_as_float(raw[k]) * sk);
-            if (lane == 0) red[warp * 64 + c * 16 + k] = s;
+            if (lane == 0) red[warp * 32 + c * 16 + k] = s;
           }
         }
         wg_sync(wg);
         if (tl < mine * 16) {
           const float old = -neg_m[tl];
-          float m = fmaxf(fmaxf(red[tl], red[64 + tl]), fmaxf(red[128 + tl], red[192 + tl]));
+          float m = fmaxf(fmaxf(red[tl], red[32 + tl]), fmaxf(red[64 + tl], red[96 + tl]));
           m = fmaxf(fmaf(fabsf(m), 0x1p-22f, m), old);  // a little above, so that no rounding leaves a positive argument
           fac[tl] = old == -kNoRef ? 1.f : ex2f(old - m);  // (no reference yet: sums and O are zero)
           neg_m[tl] = -m;
@@ -352,16 +350,19 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
       tc_fence_before();
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(S.bar(C::PVFULL + buf));
+    arrive_lane0(S.bar(C::PVFULL + buf), lane);
   }
-  // ---- row sums over the lanes: exchange halves until lane k of a warp holds the sum of row k of a 32-row group
+  // ---- row sums over the lanes: exchange halves until lane k of a warp (16 rows: and lane k + 16) holds the sum of row k
+  {
+    float v[C::kCols];
 #pragma unroll
-  for (int h = 0; h < (C::kChunks + 1) / 2; ++h) {
-    float v[32];
+    for (int k = 0; k < C::kCols / 2; ++k) unpack2(l2[k], v[2 * k], v[2 * k + 1]);
+    if (C::kCols == 16) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) unpack2(l2[h * 16 + k], v[2 * k], v[2 * k + 1]);
+      for (int k = 0; k < 16; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], 16);
+    }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
+    for (int off = C::kCols / 2; off > 0; off >>= 1) {
       const bool up = (lane & off) != 0;
 #pragma unroll
       for (int k = 0; k < off; ++k) {
@@ -369,11 +370,11 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
         v[k] = keep + __shfl_xor_sync(0xffffffffu, give, off);
       }
     }
-    red[warp * 64 + h * 32 + lane] = v[0];
+    if (lane < C::kCols) red[warp * 32 + lane] = v[0];
   }
   wg_sync(wg);
   if (tl < mine * 16) {
-    const float L = (red[tl] + red[64 + tl]) + (red[128 + tl] + red[192 + tl]);
+    const float L = (red[tl] + red[32 + tl]) + (red[64 + tl] + red[96 + tl]);
     const float M = neg_m[tl] == kNoRef ? -INFINITY : -neg_m[tl];
     const int v = c0 * 16 + tl;
     fac[tl] = L == 0.f ? 0.f : 1.f / L;
@@ -442,7 +443,7 @@ __device__ __forceinline__ void issue_pv(const Shared& S, uint32_t idesc, bool a
 }
 
 template <int RMAX>
-__global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const QuantParams P) {
+__global__ void __launch_bounds__(Cfg<RMAX>::kThreads, 1) attn_quant_kernel(const QuantParams P) {
   using C = Cfg<RMAX>;
   extern __shared__ __align__(1024) uint8_t smem[];
   Shared S;
@@ -458,20 +459,20 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     for (int i = 0; i < C::kStages; ++i) { mbar_init(S.bar(C::FULL + i), 1); mbar_init(S.bar(C::EMPTY + i), 8); }
     for (int i = 0; i < C::kA; ++i) mbar_init(S.bar(C::KFULL + i), 4);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(S.bar(C::SFULL + i), 1 + 4); mbar_init(S.bar(C::PVFULL + i), 8 + 4); mbar_init(S.bar(C::ODONE + i), 1);
+      mbar_init(S.bar(C::SFULL + i), 1 + 4); mbar_init(S.bar(C::PVFULL + i), 4 * C::kGroups + 4); mbar_init(S.bar(C::ODONE + i), 1);
       mbar_init(S.bar(C::QFULL + i), 1); mbar_init(S.bar(C::QFREE + i), 1);
     }
-    mbar_init(S.bar(C::OFREE), 8);
-    for (int i = 0; i < kSegRing; ++i) { mbar_init(S.bar(C::SEGFULL + i), 1); mbar_init(S.bar(C::SEGFREE + i), kSegReaders); }
+    mbar_init(S.bar(C::OFREE), 4 * C::kGroups);
+    for (int i = 0; i < kSegRing; ++i) { mbar_init(S.bar(C::SEGFULL + i), 1); mbar_init(S.bar(C::SEGFREE + i), C::kSegReaders); }
     *S.abort_flag = (S.base & 1023u) ? 1 : 0;  // the swizzled layouts assume a 1 KiB aligned window
     *reinterpret_cast<volatile unsigned long long*>(S.abort_flag + 2) = P.wait_ns;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   {  // zero Q, P and the ring: what a ragged tile leaves of them has to be finite
     uint4* z = reinterpret_cast<uint4*>(smem);
-    for (int i = threadIdx.x; i < C::kSmBar / 16; i += kQuantThreads) z[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < C::kSmBar / 16; i += C::kThreads) z[i] = make_uint4(0, 0, 0, 0);
   }
-  if (warp == 16) {
+  if (warp == C::kSoftmaxEnd) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
   if (P.B <= kMaxSmemPrefixSlots) {
     int* sm_prefix = reinterpret_cast<int*>(smem + C::kSmPrefix);
     int* sm_slot = reinterpret_cast<int*>(smem + C::kSmSlot);
-    block_tile_prefix<kQuantSegCost, kQuantThreads>(P, sm_prefix, sm_slot, reinterpret_cast<int*>(smem + C::kSmRed), cta == 0);
+    block_tile_prefix<kQuantSegCost, C::kThreads>(P, sm_prefix, sm_slot, reinterpret_cast<int*>(smem + C::kSmRed), cta == 0);
     prefix = sm_prefix;
     slot_info = sm_slot;
   }
@@ -519,27 +520,22 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
                      "f"(__uint_as_float(lds_u16(src + in_meta) << 16) * P.scale2), "f"(__uint_as_float(lds_u16(src + in_meta + 64) << 16)) : "memory");
         const uint32_t tk = C::kTmK + a * 64 + lane_base;
 #pragma unroll 1
-        for (uint32_t h = 0; h < 2; ++h) {
-          uint32_t o[32];
+        for (uint32_t h = 0; h < 4; ++h) {
+          uint32_t o[16];
+          const uint4 w = lds128(src + in_k + h * 256);
+          const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const uint4 w = lds128(src + in_k + h * 512 + c * 256);
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+          for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[c * 16 + u * 4 + e] = sub_zero(codes_to_bf16(ww[u] >> (4 * e)), z);
-          }
-          TMEM_ST32(tk + h * 32, o, 0);
+            for (int e = 0; e < 4; ++e) o[u * 4 + e] = sub_zero(codes_to_bf16(ww[u] >> (4 * e)), z);
+          TMEM_ST16(tk + h * 16, o, 0);
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(S.bar(C::SFULL + (n & 1u)));
-          mbar_arrive(S.bar(C::KFULL + a));
-          mbar_arrive(S.bar(C::EMPTY + s));
-        }
+        arrive_lane0(S.bar(C::SFULL + (n & 1u)), lane);
+        arrive_lane0(S.bar(C::KFULL + a), lane);
+        arrive_lane0(S.bar(C::EMPTY + s), lane);
         if (++s == C::kStages) { s = 0; full_parity ^= 1u; }
       }
     }
@@ -577,14 +573,12 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(S.bar(C::PVFULL + (n & 1u)));
-          mbar_arrive(S.bar(C::EMPTY + s));
-        }
+        arrive_lane0(S.bar(C::PVFULL + (n & 1u)), lane);
+        arrive_lane0(S.bar(C::EMPTY + s), lane);
         if (++s == C::kStages) { s = 0; full_parity ^= 1u; }
       }
     }
-  } else if (warp < 16) {
+  } else if (warp < C::kSoftmaxEnd) {
     // =========================================================================== softmax / epilogue
     regs_inc<C::kRegsSoftmax>();
     uint32_t n = 0;
@@ -592,7 +586,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
     for (uint32_t seg = 0; ok && take_segment<C>(S, seg, sg); ++seg) ok = softmax_segment_q<RMAX>(P, sg, S, (warp - 8) >> 2, n);
   } else {
     regs_dec<C::kRegsRest>();
-    if (warp == 16) {
+    if (warp == C::kSoftmaxEnd) {
     // =========================================================================== page copies
     uint32_t n = 0;
     bool ok = true;
@@ -628,7 +622,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
       for (uint32_t f = (n > (uint32_t)C::kStages ? n - C::kStages : 0); f < n; ++f)
         isd_bounded_wait(P.wait_ns, nullptr, [&]() { return mbar_try_wait(S.bar(C::FULL + f % C::kStages), (f / C::kStages) & 1u); });
     }
-    } else if (warp == 17) {
+    } else if (warp == C::kSoftmaxEnd + 1) {
     // =========================================================================== QK issuer: one thread from here on
     if (elect_one()) {
       uint32_t n = 0;
@@ -650,7 +644,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
       }
     }
     __syncwarp();
-    } else if (warp == 18) {
+    } else if (warp == C::kSoftmaxEnd + 2) {
     // =========================================================================== PV issuer: one thread
     if (elect_one()) {
       uint32_t n = 0;
@@ -710,7 +704,7 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *S.abort_flag) atomicOr(P.global_status, ISD_ST_KERNEL_TIMEOUT);
-  if (warp == 16) {
+  if (warp == C::kSoftmaxEnd) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(S.tmem) : "memory");
   }
@@ -718,14 +712,15 @@ __global__ void __launch_bounds__(kQuantThreads, 1) attn_quant_kernel(const Quan
 
 template <int RMAX>
 cudaError_t launch_main(const QuantParams& P, cudaStream_t stream) {
-  return isd_launch_pdl(attn_quant_kernel<RMAX>, dim3(P.num_ctas), dim3(kQuantThreads), Cfg<RMAX>::kSmemBytes, stream, P);
+  return isd_launch_pdl(attn_quant_kernel<RMAX>, dim3(P.num_ctas), dim3(Cfg<RMAX>::kThreads), Cfg<RMAX>::kSmemBytes, stream, P);
 }
 
 }  // namespace
 
 int isd_attn_quant_create(isd_ctx* ctx) {
   if (cudaMalloc(&ctx->quant_prefix, sizeof(int) * (ctx->cfg.batch + 1)) != cudaSuccess) return ISD_ERR_NO_MEMORY;
-  if (cudaFuncSetAttribute(attn_quant_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes) != cudaSuccess ||
+  if (cudaFuncSetAttribute(attn_quant_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<32>::kSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(attn_quant_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes) != cudaSuccess ||
       cudaFuncSetAttribute(attn_quant_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmemBytes) != cudaSuccess)
     return ISD_ERR_CUDA;
   return ISD_OK;
@@ -750,7 +745,7 @@ int isd_launch_attn_quant(isd_ctx* ctx, const isd_batch_state* st, const void* q
   cudaError_t e = cudaSuccess;
   if (c.batch > kMaxSmemPrefixSlots) e = isd_launch_pdl(attn_plan_kernel<kQuantSegCost>, dim3(1), dim3(1024), 0, stream, P);
   if (ctx->ev_attn0) cudaEventRecord(ctx->ev_attn0, stream);
-  if (e == cudaSuccess) e = ctx->G * ctx->Q <= 64 ? launch_main<64>(P, stream) : launch_main<128>(P, stream);
+  if (e == cudaSuccess) e = ctx->G * ctx->Q <= 32 ? launch_main<32>(P, stream) : ctx->G * ctx->Q <= 64 ? launch_main<64>(P, stream) : launch_main<128>(P, stream);
   if (ctx->ev_attn1) cudaEventRecord(ctx->ev_attn1, stream);
   if (e == cudaSuccess) e = isd_launch_pdl(attn_combine_kernel<kQuantSegCost, false>, dim3(P.num_ctas), dim3(kCombineThreads), 0, stream, P);
   ctx->launches += 2 + (c.batch > kMaxSmemPrefixSlots ? 1 : 0);
