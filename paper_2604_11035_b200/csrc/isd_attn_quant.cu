@@ -21,9 +21,9 @@
 // (probabilities are then at most 2^8, far from any limit of fp32 or bf16, whose precision does not depend on magnitude): a
 // tile costs one vote of the warpgroup.  Row sums stay in registers per lane and are reduced over lanes once a segment.
 //
-// Warps: 0-3 decode K, 4-7 decode V, 8-11 and 12-15 softmax and epilogue of one half of the rows each, 16 and 18 copy pages
-// (one bulk copy of 2176 bytes holds K and V of a (page, head)), 17 issues the MMAs, 19 works out the CTA's segments and
-// stages their Q.  Work split and combine pass: isd_attn_split.cuh.  Every wait is bounded, as in the bf16 kernel.
+// Warps: 0-3 decode K, 4-7 decode V, then two or four warpgroups do softmax and epilogue of a share of the rows each, then one
+// warp each copies pages (one bulk copy of 2176 bytes holds K and V of a (page, head)), issues QK^T, issues PV, and works out
+// the CTA's segments and stages their Q.  Work split and combine pass: isd_attn_split.cuh.  Every wait is bounded, as in the bf16 kernel.
 #include <new>
 
 #include "isd_attn_split.cuh"
@@ -34,6 +34,7 @@ namespace {
 constexpr int kStageQ = 8 * kQTile;    // one tile of 128 keys: eight pages' tiles
 constexpr int kQuantSegCost = 4;       // fixed cost of a segment in units of one tile's time
 constexpr float kNoRef = 3.0e38f;      // any score plus this asks for a reference; a masked one (-inf) does not
+constexpr float kLarge = 0x1p20f;      // references from here on are exact maxima of rounded scores
 constexpr int kScaleBufs = 4;          // the decoders run at most three tiles ahead of the softmax
 constexpr int kSegRing = 4;
 
@@ -223,6 +224,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
   wg_sync(wg);
   const uint32_t to = S.tmem + C::kTmO + (uint32_t)c0 * 16 + lane_base;
   const uint32_t sw = ((uint32_t)tl & 7u) << 4, p_row = S.base + C::kSmP + (uint32_t)tl * 128;
+  bool large = false;  // some row's reference has passed kLarge
   for (int i = 0; i < cnt; ++i) {
     const uint32_t nn = n + (uint32_t)i, buf = nn & 1u;
     if (!S.wait(C::SFULL + buf, nn >> 1)) return false;
@@ -231,31 +233,11 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
     if (mine > 0) {
       tc_fence_after();
       const uint32_t ts = S.tmem + C::kTmS + buf * RMAX + (uint32_t)c0 * 16 + lane_base;
-      // Tiles that reach into the block: the scores go back to tensor memory with -inf where the row does not see the key (and
-      // NaN where it does and the value scale is NaN, which then needs no factor), so that all other tiles are spared the masks.
-      if ((sg.j0 + i + 1) * kTile > sg.ctx) {
-        // rows v < vmin do not see this lane's key (row v of the packed block is block row v / G)
-        const int key = (sg.j0 + i) * kTile + tl;
-        const int vmin = key >= sg.kv_len ? 0x7FFFFFFF : (key > sg.ctx ? (key - sg.ctx) * P.G : 0);
-        const bool bad_sv = sv != sv;
-        const float add = bad_sv ? sv : 0.f;
-#pragma unroll 1
-        for (int c = 0; c < mine; ++c) {
-          uint32_t raw[16];
-          tmem_ld16(ts + c * 16, raw);
-#pragma unroll
-          for (int k = 0; k < 16; ++k)
-            raw[k] = (c0 + c) * 16 + k < vmin ? 0xFF800000u : __float_as_uint(fmaf(__uint_as_float(raw[k]), sk, add));
-          TMEM_ST16(ts + c * 16, raw, 0);
-        }
-        tmem_wait_st();
-        sk = 1.f;
-        if (bad_sv || vmin == 0x7FFFFFFF) sv = 0.f;
-      }
-      const uint64_t sk2 = pack2(sk, sk), sv2 = pack2(sv, sv);
+      bool rewrite = large || (sg.j0 + i + 1) * kTile > sg.ctx;
       // ---- arguments x = score (log2 domain) - reference; does any pass 8?
       uint64_t x2[kKeep ? C::kChunks * 8 : 8];
       auto arguments = [&](int c, uint64_t* x) -> float {
+        const uint64_t sk2 = pack2(sk, sk);
         uint32_t raw[16];
         const uint4 m0 = lds128(neg_m_a + c * 64), m1 = lds128(neg_m_a + c * 64 + 16), m2 = lds128(neg_m_a + c * 64 + 32), m3 = lds128(neg_m_a + c * 64 + 48);
         tmem_ld16(ts + c * 16, raw);
@@ -274,6 +256,25 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
                      max3(max3(b[4], a[5], b[5]), max3(a[6], b[6], a[7]), b[7]));
       };
       for (int raised = 0;; ++raised) {
+        // Tiles that reach into the block: the scores go back to tensor memory scaled, with -inf where the row does not see the
+        // key, so that all other tiles are spared the masks.  So do those of rows with a large reference: a score's rounding is
+        // then no longer small beside 1, and only scores that were rounded before they are compared are none above their maximum.
+        if (rewrite) {
+          // rows v < vmin do not see this lane's key (row v of the packed block is block row v / G)
+          const int key = (sg.j0 + i) * kTile + tl;
+          const int vmin = key >= sg.kv_len ? 0x7FFFFFFF : (key > sg.ctx ? (key - sg.ctx) * P.G : 0);
+#pragma unroll 1
+          for (int c = 0; c < mine; ++c) {
+            uint32_t raw[16];
+            tmem_ld16(ts + c * 16, raw);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) raw[k] = (c0 + c) * 16 + k < vmin ? 0xFF800000u : __float_as_uint(__uint_as_float(raw[k]) * sk);
+            TMEM_ST16(ts + c * 16, raw, 0);
+          }
+          tmem_wait_st();
+          sk = 1.f;
+          if (vmin == 0x7FFFFFFF) sv = 0.f;
+        }
         float mx = -INFINITY;
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c)
@@ -292,14 +293,19 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
           }
         }
         wg_sync(wg);
+        bool grown = false;
         if (tl < mine * 16) {
           const float old = -neg_m[tl];
           float m = fmaxf(fmaxf(red[tl], red[32 + tl]), fmaxf(red[64 + tl], red[96 + tl]));
-          m = fmaxf(fmaf(fabsf(m), 0x1p-22f, m), old);  // a little above, so that no rounding leaves a positive argument
+          grown = fabsf(m) >= kLarge && m != -INFINITY;
+          if (!grown) m = fmaf(fabsf(m), 0x1p-22f, m);  // a little above, so that no rounding leaves a positive argument
+          m = fmaxf(m, old);
           fac[tl] = old == -kNoRef ? 1.f : ex2f(old - m);  // (no reference yet: sums and O are zero)
           neg_m[tl] = -m;
         }
-        wg_sync(wg);
+        grown = wg_any(wg, grown);
+        rewrite = grown && !rewrite;  // (this tile as well, if it was not)
+        large = large || grown;
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c)
           if (c < mine) {
@@ -338,7 +344,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
             unpack2(x[k], a, b);
             const uint64_t p = pack2(ex2f(a), ex2f(b));
             l2[c * 8 + k] = add2(l2[c * 8 + k], p);
-            unpack2(mul2(p, sv2), a, b);
+            unpack2(mul2(p, pack2(sv, sv)), a, b);
             pk[k] = pack_bf16_cvt(a, b);
           }
           const int cc = c0 + c;
@@ -346,6 +352,13 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
           sts128(row + (u ^ sw), pk[0], pk[1], pk[2], pk[3]);
           sts128(row + ((u + 16) ^ sw), pk[4], pk[5], pk[6], pk[7]);
         }
+      if (sv != sv && (sg.j0 + i + 1) * kTile > sg.ctx) {  // a NaN value scale, times the zeros of rows that do not see the key
+        const int unseen = ((sg.j0 + i) * kTile + tl - sg.ctx) * P.G;
+#pragma unroll 1
+        for (int v = c0 * 16; v < min(unseen, (c0 + mine) * 16); ++v)
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(p_row + buf * C::kPBytes + (uint32_t)(v >> 6) * 16384 + (((uint32_t)(v & 63) * 2) ^ sw)), "h"((uint16_t)0)
+                       : "memory");
+      }
       fence_async_smem();
       tc_fence_before();
     }

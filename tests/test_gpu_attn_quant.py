@@ -205,6 +205,53 @@ def test_a_nan_in_the_cache_reaches_those_who_see_it_alone():
     assert not torch.isnan(lse[0, :2]).any() and not torch.isnan(lse[0, :, 4:]).any()
 
 
+@pytest.mark.parametrize("stride", [1, 4, 16])
+def test_a_nan_value_scale_spoils_outputs_and_no_log_sums(stride):
+    """One in the cached part (all rows see it), one in the block (rows from its own on)."""
+    p = Problem([300, 200], [0, 0], stride, 8, 2, seed=17)
+    clean = Problem([300, 200], [0, 0], stride, 8, 2, seed=17).to_gpu()
+    clean.call()
+    p.cache.s[1, p.table[0, 3], 1, 5] = np.nan
+    p.v_new[1, stride - 1, 0, 7] = float("nan")
+    p.to_gpu()
+    p.call()
+    out, lse = p.out.float(), p.lse
+    assert torch.equal(lse[:, :stride], clean.lse[:, :stride])
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[0, :stride, 4:] = True
+    bad[1, stride - 1, :4] = True
+    assert torch.equal(torch.isnan(out), bad)
+    assert torch.equal(p.out[~bad], clean.out[~bad])
+
+
+@pytest.mark.parametrize("stride", [1, 4, 16])
+@pytest.mark.parametrize("power", [28, 60, 100])
+def test_scores_far_beyond_any_probability(power, stride):
+    """The largest score takes all the weight: its lead over the second (checked here) is far above the rounding of the scores, an
+    fp32 sum of 128 products (129 * 2^-24 of the sum of magnitudes)."""
+    p = Problem([500], [0], stride, 8, 2, seed=18)
+    p.cache.s[0] *= 2.0 ** power
+    p.k_new = (p.k_new.float() * 2.0 ** power).bfloat16()
+    p.to_gpu()
+    p.call()
+    assert p.isd.isd_read_status() == 0
+    K, W, n = p.slot_values(0)
+    out, lse = p.out.double().cpu().numpy(), p.lse.double().cpu().numpy()
+    x = p.q[0].double().numpy()
+    checked = 0
+    for r in range(n):
+        for h in range(8):
+            a, mag = K[h // 4, :500 + r + 1] @ x[r, h], np.abs(K[h // 4, :500 + r + 1]) @ np.abs(x[r, h])
+            top = np.argsort(a)[-2:]
+            err = 144 * 2.0 ** -24 * mag.max()
+            assert abs(lse[0, r, h] - a[top[1]] * p.scale) <= err * p.scale + 2.0 ** -20 * abs(a[top[1]]) * p.scale
+            if a[top[1]] - a[top[0]] > 4 * err and power >= 28:  # then the second's weight is exp(-2^6) at most
+                want = W[h // 4, top[1]]
+                assert (np.abs(out[0, r, h] - want) <= 3 * 2.0 ** -8 * np.abs(want) + 1e-20).all(), (r, h)
+                checked += 1
+    assert checked >= n * 8 * 3 // 4
+
+
 def test_a_nan_in_a_query_stays_in_its_row():
     p = Problem([300], [3], 4, 8, 2, seed=13)
     p.q[0, 3, 5, 0] = float("nan")

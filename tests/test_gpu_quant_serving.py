@@ -1,0 +1,154 @@
+"""Requests that come and go on a 4-bit cache: isd_admit, isd_kv_write_quant, isd_step_quant, isd_logprobs, isd_release (needs a B200)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_11035_b200 as isd_pkg
+from quant_ref import Cache, D, PAGE, attention, attention_bounds
+from test_gpu_logprobs import check as check_logprobs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+B, N, HQ, HKV, V, WIDTH, PAGES, LAYERS = 5, 4, 8, 2, 2048, 14, 48, 2
+Q = 2 * N - 1
+
+
+class Server:
+    """The framework's calls beside a mirror of both layers' caches."""
+
+    def __init__(self, logits_dtype, propose_mode):
+        i32 = dict(dtype=torch.int32, device=DEV)
+        self.isd = isd_pkg.Isd(batch=B, stride=N, n_q_heads=HQ, n_kv_heads=HKV, vocab=V, max_pages_per_slot=WIDTH, num_pages=PAGES,
+                               logits_dtype=logits_dtype, propose_mode=propose_mode, q_mode=1, seed=7)
+        self.dtype = torch.float32 if logits_dtype == "f32" else torch.bfloat16
+        self.st = dict(ctx_len=torch.zeros(B, **i32), n_ver=torch.zeros(B, **i32), block_tok=torch.zeros(B, Q, **i32), q_row0=torch.zeros(B, **i32),
+                       q_stats=torch.zeros(B, N - 1, 2, device=DEV), page_table=torch.full((B, WIDTH), -1, **i32),
+                       free_stack=torch.randperm(PAGES, generator=torch.Generator().manual_seed(3)).to(**i32), free_top=torch.full((1,), PAGES, **i32),
+                       active=torch.zeros(B, dtype=torch.uint8, device=DEV), slot_status=torch.zeros(B, **i32))
+        self.pools = [isd_pkg.alloc_kv_pool_quant(PAGES, HKV, DEV) for _ in range(LAYERS)]
+        self.caches = [Cache(PAGES, HKV) for _ in range(LAYERS)]
+        self.out = isd_pkg.alloc_verify_out(B, N, DEV)
+        self.g = torch.Generator().manual_seed(11)
+        self.prev, self.t = None, 0
+
+    def normal(self, *s):
+        return torch.randn(*s, generator=self.g).bfloat16()
+
+    def admit(self, slots, lens):
+        t = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+        maps = isd_pkg.alloc_admit_maps(len(slots), 512, DEV)
+        maps["slot_map"].fill_(-1)  # (padding)
+        self.isd.isd_admit(self.st, t(slots), t(lens), t([5] * len(slots)), maps)
+        assert maps["result"].tolist() == [0] * len(slots)
+        rows = self.normal(LAYERS, 2, 512, HKV, D)
+        where = maps["slot_map"].cpu().tolist()
+        for layer in range(LAYERS):
+            k, v = rows[layer].to(DEV)
+            self.isd.isd_kv_write_quant(k, v, maps["slot_map"], self.pools[layer])
+            for i, s in enumerate(where):
+                if s >= 0:
+                    self.caches[layer].store(s // PAGE, s % PAGE, rows[layer, 0, i].float().numpy(), rows[layer, 1, i].float().numpy())
+            back = [torch.full((512, HKV, D), 9.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+            self.isd.isd_kv_read_quant(self.pools[layer], maps["slot_map"], *back)
+            for got, mirror in zip(back, range(2)):
+                for i, s in enumerate(where):
+                    want = self.caches[layer].values(s // PAGE)[mirror][:, s % PAGE] if s >= 0 else np.full((HKV, D), 9.0)
+                    assert np.array_equal(got[i].float().cpu().numpy(), torch.from_numpy(want).bfloat16().float().numpy())
+
+    def step(self):
+        s = {k: v.cpu().numpy().copy() for k, v in self.st.items()}
+        x = [(self.normal(B, Q, HQ, D), self.normal(B, Q, HKV, D), self.normal(B, Q, HKV, D)) for _ in range(LAYERS)]
+        att = [torch.full((B, Q, HQ, D), 77.0, dtype=torch.bfloat16, device=DEV) for _ in range(LAYERS)]
+        lse = [torch.full((B, Q, HQ), 77.0, device=DEV) for _ in range(LAYERS)]
+        logits = (torch.randn(B, Q, V, generator=self.g) * 2).to(self.dtype)
+        logits[:, :, 100 + self.t] += 9.0  # (proposals and verified rows mostly agree from one step to the next)
+        logits[:, :, 101 + self.t] += 9.0
+        logits = logits.to(DEV)
+        keep = [[a.to(DEV) for a in row] for row in x]
+        layers = self.isd.quant_layer_args([dict(q=keep[i][0], k_new=keep[i][1], v_new=keep[i][2], kv_pool=self.pools[i], attn_out=att[i],
+                                                 attn_lse=lse[i]) for i in range(LAYERS)])
+        self.isd.isd_step_quant(self.st, layers, logits, self.prev, self.out, self.t)
+        assert self.isd.isd_read_status() == 0
+        # ---- attention of every layer
+        for i in range(LAYERS):
+            o, l = att[i].double().cpu().numpy(), lse[i].double().cpu().numpy()
+            for b in range(B):
+                if not s["active"][b]:
+                    assert (o[b] == 77).all() and (l[b] == 77).all()
+                    continue
+                n, ctx, tab = int(s["n_ver"][b]) + N, int(s["ctx_len"][b]), s["page_table"][b]
+                for r in range(n):
+                    self.caches[i].store(tab[(ctx + r) // PAGE], (ctx + r) % PAGE, x[i][1][b, r].float().numpy(), x[i][2][b, r].float().numpy())
+                pages = [self.caches[i].values(p) for p in tab[:(ctx + n + PAGE - 1) // PAGE]]
+                K, W = (np.concatenate([p[j] for p in pages], 1) for j in range(2))
+                want, wl, absv, mag = attention(x[i][0][b, :n].double().numpy(), K, W, ctx, 1 / np.sqrt(D))
+                to, tl = attention_bounds(want, wl, absv, mag)
+                assert (np.abs(o[b, :n] - want) <= to).all() and (np.abs(l[b, :n] - wl) <= tl).all(), (self.t, i, b)
+                assert (o[b, n:] == 77).all() and (l[b, n:] == 77).all()
+        # ---- log probabilities of the emitted tokens: token i of a slot came from its block's row i
+        live = torch.from_numpy(s["active"].astype(bool)).to(DEV)
+        tokens = torch.where((torch.arange(N, device=DEV) < self.out["n_emit"][:, None]) & live[:, None], self.out["out_tok"], -1).int().reshape(-1)
+        rows = (torch.arange(B, device=DEV)[:, None] * Q + torch.arange(N, device=DEV)).int().reshape(-1).contiguous()
+        got = check_logprobs(self.isd, logits, tokens, rows=rows, top=4)
+        emitted = int(self.out["n_emit"][live].sum())
+        assert int(torch.isfinite(got["logprob"]).sum()) == emitted >= int(live.sum())
+        assert np.array_equal(self.st["ctx_len"].cpu().numpy()[s["active"] > 0], (s["ctx_len"] + self.out["n_emit"].cpu().numpy())[s["active"] > 0])
+        self.prev, self.t = logits, self.t + 1
+
+    def pages_are_all_there(self):
+        s = {k: v.cpu().numpy() for k, v in self.st.items()}
+        held = [int(p) for b in range(B) if s["active"][b] for p in s["page_table"][b, :(s["ctx_len"][b] + Q + PAGE - 1) // PAGE]]
+        assert sorted(held + s["free_stack"][:s["free_top"][0]].tolist()) == list(range(PAGES))
+
+
+@pytest.mark.parametrize("logits_dtype,propose_mode", [("f32", 1), ("bf16", 0)])
+def test_requests_come_and_go(logits_dtype, propose_mode):
+    s = Server(logits_dtype, propose_mode)
+    s.admit([3, 0], [33, 0])
+    s.step()
+    s.admit([4, 1, 2], [16, 150, 1])
+    for _ in range(3):
+        s.step()
+        s.pages_are_all_there()
+    s.isd.isd_release(s.st, torch.tensor([1, 3], dtype=torch.int32, device=DEV))
+    s.pages_are_all_there()
+    s.step()
+    s.admit([1], [130])  # into pages and a slot that others used before
+    for _ in range(2):
+        s.step()
+        s.pages_are_all_there()
+
+
+def test_a_captured_step_with_log_probabilities_replays_like_eager_calls():
+    """The state goes through the same steps whether the calls run one by one or from a graph."""
+    seen = []
+    for captured in (False, True):
+        s = Server("f32", 1)
+        s.admit([0, 2, 4], [20, 47, 3])
+        counter = torch.zeros(1, dtype=torch.int32, device=DEV)
+        s.isd.isd_set_step_counter(counter)
+        q, k, v = (s.normal(B, Q, h, D).to(DEV) for h in (HQ, HKV, HKV))
+        lg = (torch.randn(B, Q, V, generator=s.g) * 2).to(DEV)
+        att = [torch.zeros(B, Q, HQ, D, dtype=torch.bfloat16, device=DEV) for _ in range(LAYERS)]
+        layers = s.isd.quant_layer_args([dict(q=q, k_new=k, v_new=v, kv_pool=s.pools[i], attn_out=att[i]) for i in range(LAYERS)])
+        rows = (torch.arange(B, device=DEV)[:, None] * Q + torch.arange(N, device=DEV)).int().reshape(-1).contiguous()
+        lp = isd_pkg.alloc_logprobs_out(B * N, 3, DEV)
+
+        def calls():
+            s.isd.isd_step_quant(s.st, layers, lg, lg, s.out, 0)
+            s.isd.isd_logprobs(lg, s.out["out_tok"].reshape(-1), rows=rows, top_n=3, out=lp)
+
+        s.out["out_tok"].fill_(-1)
+        calls()
+        if captured:
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                calls()
+        for _ in range(3):
+            graph.replay() if captured else calls()
+        torch.cuda.synchronize()
+        assert s.isd.isd_read_status() == 0 and int(counter) == 4
+        seen.append([s.out[n].clone() for n in ("n_emit", "out_tok", "accept_len")] + [s.st[n].clone() for n in ("ctx_len", "n_ver", "block_tok", "page_table")]
+                    + [*att, *s.pools] + [torch.nan_to_num(lp[n], nan=-123.0) for n in ("logprob", "entropy", "top_logprob")] + [lp["top_id"]])
+    assert all(torch.equal(a, b) for a, b in zip(*seen))
