@@ -233,7 +233,28 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
     if (mine > 0) {
       tc_fence_after();
       const uint32_t ts = S.tmem + C::kTmS + buf * RMAX + (uint32_t)c0 * 16 + lane_base;
-      bool rewrite = large || (sg.j0 + i + 1) * kTile > sg.ctx;
+      // Tiles that reach into the block: the scores go back to tensor memory scaled, with -inf where the row does not see the
+      // key, so that all other tiles are spared the masks.  So do those of rows with a large reference: a score's rounding is
+      // then no longer small beside 1, and only scores that were rounded before they are compared are none above their maximum.
+      bool spoiled = false;
+      const bool rewrite = large || (sg.j0 + i + 1) * kTile > sg.ctx;
+      if (rewrite) {
+        // rows v < vmin do not see this lane's key (row v of the packed block is block row v / G)
+        const int key = (sg.j0 + i) * kTile + tl;
+        const int vmin = key >= sg.kv_len ? 0x7FFFFFFF : (key > sg.ctx ? (key - sg.ctx) * P.G : 0);
+#pragma unroll 1
+        for (int c = 0; c < mine; ++c) {
+          uint32_t raw[16];
+          tmem_ld16(ts + c * 16, raw);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) raw[k] = (c0 + c) * 16 + k < vmin ? 0xFF800000u : __float_as_uint(__uint_as_float(raw[k]) * sk);
+          TMEM_ST16(ts + c * 16, raw, 0);
+        }
+        tmem_wait_st();
+        sk = 1.f;
+        if (vmin == 0x7FFFFFFF) sv = 0.f;
+        spoiled = sv != sv && vmin > 0;
+      }
       // ---- arguments x = score (log2 domain) - reference; does any pass 8?
       uint64_t x2[kKeep ? C::kChunks * 8 : 8];
       auto arguments = [&](int c, uint64_t* x) -> float {
@@ -256,25 +277,6 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
                      max3(max3(b[4], a[5], b[5]), max3(a[6], b[6], a[7]), b[7]));
       };
       for (int raised = 0;; ++raised) {
-        // Tiles that reach into the block: the scores go back to tensor memory scaled, with -inf where the row does not see the
-        // key, so that all other tiles are spared the masks.  So do those of rows with a large reference: a score's rounding is
-        // then no longer small beside 1, and only scores that were rounded before they are compared are none above their maximum.
-        if (rewrite) {
-          // rows v < vmin do not see this lane's key (row v of the packed block is block row v / G)
-          const int key = (sg.j0 + i) * kTile + tl;
-          const int vmin = key >= sg.kv_len ? 0x7FFFFFFF : (key > sg.ctx ? (key - sg.ctx) * P.G : 0);
-#pragma unroll 1
-          for (int c = 0; c < mine; ++c) {
-            uint32_t raw[16];
-            tmem_ld16(ts + c * 16, raw);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) raw[k] = (c0 + c) * 16 + k < vmin ? 0xFF800000u : __float_as_uint(__uint_as_float(raw[k]) * sk);
-            TMEM_ST16(ts + c * 16, raw, 0);
-          }
-          tmem_wait_st();
-          sk = 1.f;
-          if (vmin == 0x7FFFFFFF) sv = 0.f;
-        }
         float mx = -INFINITY;
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c)
@@ -304,8 +306,19 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
           neg_m[tl] = -m;
         }
         grown = wg_any(wg, grown);
-        rewrite = grown && !rewrite;  // (this tile as well, if it was not)
         large = large || grown;
+        if (grown && !rewrite) {  // this tile as well
+#pragma unroll 1
+          for (int c = 0; c < mine; ++c) {
+            uint32_t raw[16];
+            tmem_ld16(ts + c * 16, raw);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) raw[k] = __float_as_uint(__uint_as_float(raw[k]) * sk);
+            TMEM_ST16(ts + c * 16, raw, 0);
+          }
+          tmem_wait_st();
+          sk = 1.f;
+        }
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c)
           if (c < mine) {
@@ -352,7 +365,7 @@ __device__ __forceinline__ bool softmax_segment_q(const QuantParams& P, const Se
           sts128(row + (u ^ sw), pk[0], pk[1], pk[2], pk[3]);
           sts128(row + ((u + 16) ^ sw), pk[4], pk[5], pk[6], pk[7]);
         }
-      if (sv != sv && (sg.j0 + i + 1) * kTile > sg.ctx) {  // a NaN value scale, times the zeros of rows that do not see the key
+      if (spoiled) {  // a NaN value scale, times the zeros of rows that do not see the key
         const int unseen = ((sg.j0 + i) * kTile + tl - sg.ctx) * P.G;
 #pragma unroll 1
         for (int v = c0 * 16; v < min(unseen, (c0 + mine) * 16); ++v)
