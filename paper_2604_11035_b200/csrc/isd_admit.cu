@@ -4,7 +4,7 @@
 // writes page tables and the tokens' maps.
 #include <limits.h>
 
-#include "isd_commit.cuh"
+#include "isd_internal.cuh"
 
 namespace {
 
@@ -36,8 +36,39 @@ struct AdmitParams {
 
 constexpr int kAdmitThreads = 1024;
 
+struct Pair {
+  int64_t a, b;
+};
+// exclusive prefix sums of two quantities over the block, and their totals (64 bits: 1024 requests may ask for more than 2^31
+// pages or tokens).  Every thread calls; sm: one Pair per warp and one more.
+__device__ __forceinline__ Pair block_scan(Pair v, Pair* sm, Pair& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto warp_scan = [&](Pair x) {
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int64_t a = __shfl_up_sync(0xffffffffu, x.a, off), b = __shfl_up_sync(0xffffffffu, x.b, off);
+      if (lane >= off) { x.a += a; x.b += b; }
+    }
+    return x;
+  };
+  const Pair inc = warp_scan(v);
+  if (lane == 31) sm[warp] = inc;
+  __syncthreads();
+  if (warp == 0) {
+    const Pair w = sm[lane], winc = warp_scan(w);
+    __syncwarp();
+    sm[lane] = {winc.a - w.a, winc.b - w.b};
+    if (lane == 31) sm[32] = winc;
+  }
+  __syncthreads();
+  const Pair base = sm[warp];
+  total = sm[32];
+  __syncthreads();
+  return {base.a + inc.a - v.a, base.b + inc.b - v.b};
+}
+
 __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitParams P) {
-  __shared__ int sm_warp[33];
+  __shared__ Pair sm[kAdmitThreads / 32 + 1];
   pdl_wait();
   pdl_launch_dependents();
   // the first request of a slot counts
@@ -67,24 +98,20 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
       }
     }
     const bool asks = i < P.n && !why;
-    // (a round asks for at most 1024 requests; sums in 64 bits over the two halves of a length)
-    int tp, tl, th;
-    const int64_t before_p = pages0 + block_exclusive_scan(asks ? want : 0, sm_warp, tp);
-    const int lo = asks ? (len & 0xFFFF) : 0, hi = asks ? (len >> 16) : 0;
-    const int64_t sl = block_exclusive_scan(lo, sm_warp, tl), sh = block_exclusive_scan(hi, sm_warp, th);
-    const int64_t before_t = toks0 + sl + (sh << 16);
-    pages0 += tp;
-    toks0 += tl + ((int64_t)th << 16);
+    Pair all;
+    const Pair before = block_scan({asks ? want : 0, asks ? len : 0}, sm, all);
+    const int64_t before_p = pages0 + before.a, before_t = toks0 + before.b;
+    pages0 += all.a;
+    toks0 += all.b;
     if (asks) {
       if (before_p + want > top) why = ISD_ST_POOL_EXHAUSTED;
       else if (before_t + len > P.map_cap) why = ISD_ST_MAP_FULL;
     }
     const bool ok = asks && !why;
-    // (admitted requests are at most one per slot, so their number and the pages they take fit one scan each)
-    int n_p, n_t, n_k;
-    const int my_p = block_exclusive_scan(ok ? want : 0, sm_warp, n_p);
-    const int my_t = block_exclusive_scan(ok ? len : 0, sm_warp, n_t);
-    const int my_k = served + block_exclusive_scan(ok ? 1 : 0, sm_warp, n_k);
+    // (what is served fits the pool and the maps: pages and tokens below 2^31; the requests' number goes above the tokens)
+    const Pair took = block_scan({ok ? want : 0, ok ? len + (1ll << 32) : 0}, sm, all);
+    const int my_p = (int)took.a, my_t = (int)(took.b & 0xFFFFFFFFll), my_k = served + (int)(took.b >> 32);
+    const int n_p = (int)all.a, n_t = (int)(all.b & 0xFFFFFFFFll), n_k = (int)(all.b >> 32);
     if (i < P.n) {
       P.result[i] = (int32_t)why;
       P.cu_len[i] = served_toks + my_t;

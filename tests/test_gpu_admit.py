@@ -118,6 +118,23 @@ def test_lengths_near_the_ends_of_32_bits():
     assert want["result"].tolist() == [ST_SLOT_CAPACITY] * 3 + [0]
 
 
+def test_requests_for_more_than_two_to_the_31_pages():
+    """1024 slots of two million pages each: what a round of them asks for passes 32 bits."""
+    B, width, pages = 1100, (1 << 21) + 4096, 64
+    i32 = dict(dtype=torch.int32, device=DEV)
+    st = dict(ctx_len=torch.zeros(B, **i32), n_ver=torch.zeros(B, **i32), block_tok=torch.zeros(B, 3, **i32), q_row0=torch.zeros(B, **i32),
+              q_stats=torch.zeros(B, 1, 2, device=DEV), page_table=torch.empty(B, width, **i32), free_stack=torch.arange(pages, **i32),
+              free_top=torch.full((1,), pages, **i32), active=torch.zeros(B, dtype=torch.uint8, device=DEV), slot_status=torch.zeros(B, **i32))
+    isd = isd_pkg.Isd(batch=B, stride=2, n_q_heads=4, n_kv_heads=4, vocab=64, max_pages_per_slot=width, num_pages=pages, logits_dtype="f32")
+    lens = torch.full((B,), width * PAGE - 3, **i32)
+    lens[0], lens[1050:] = 20, 5
+    maps = isd_pkg.alloc_admit_maps(B, 100, DEV)
+    isd.isd_admit(st, torch.arange(B, **i32), lens, torch.zeros(B, **i32), maps)
+    assert maps["result"].tolist() == [0] + [ST_POOL_EXHAUSTED] * (B - 1)
+    assert int(st["free_top"]) == pages - 2 and st["active"].nonzero().flatten().tolist() == [0]
+    assert st["page_table"][0, :2].tolist() == [63, 62] and int(maps["cu_len"][B]) == 20
+
+
 def test_maps_that_are_too_short_or_left_out():
     b = Batch(8, 2, 6, 64, 60)
     _, want = b.admit([0, 1, 2], [20, 30, 5], cap=40)
