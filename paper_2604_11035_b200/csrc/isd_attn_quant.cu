@@ -705,20 +705,16 @@ __global__ void __launch_bounds__(Cfg<RMAX>::kThreads, 1) attn_quant_kernel(cons
       const uint32_t qb = S.base + C::kSmQ + (seg & 1u) * RMAX * 256;
       const __nv_bfloat16* src = P.q + ((size_t)sg.b * P.Q * P.Hq + sg.g * P.G) * ISD_HEAD_DIM;
       const int piece = lane & 15;  // 16 bytes of a row's 256
-      for (int v0 = lane >> 4; v0 < padded; v0 += 8) {  // two rows a step, four steps in flight
-        uint4 x[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int v = v0 + 2 * u;
-          x[u] = make_uint4(0, 0, 0, 0);
-          if (v < rows) x[u] = *reinterpret_cast<const uint4*>(src + ((size_t)(v / P.G) * P.Hq + v % P.G) * ISD_HEAD_DIM + piece * 8);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t v = (uint32_t)(v0 + 2 * u);
-          sts128(qb + (uint32_t)(piece >> 3) * (RMAX * 128) + v * 128 + ((((uint32_t)piece & 7u) ^ (v & 7u)) << 4), x[u].x, x[u].y, x[u].z, x[u].w);
-        }
+      // (asynchronous copies: all rows are in flight at once, so that staging takes one trip to memory)
+      int r = (lane >> 4) / P.G, hg = (lane >> 4) - r * P.G;
+      for (uint32_t v = (uint32_t)lane >> 4; (int)v < padded; v += 2) {  // two rows a step
+        const bool have = (int)v < rows;
+        const __nv_bfloat16* from = have ? src + ((size_t)r * P.Hq + hg) * ISD_HEAD_DIM + piece * 8 : src;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(qb + (uint32_t)(piece >> 3) * (RMAX * 128) + v * 128 + ((((uint32_t)piece & 7u) ^ (v & 7u)) << 4)),
+                     "l"(from), "r"(have ? 16 : 0) : "memory");
+        for (hg += 2; hg >= P.G; hg -= P.G) ++r;
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(S.bar(C::QFULL + (seg & 1u)));
