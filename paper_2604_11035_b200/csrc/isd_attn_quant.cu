@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(Cfg<RMAX>::kThreads, 1) attn_quant_kernel(cons
     int* sm_slot = reinterpret_cast<int*>(smem + C::kSmSlot);
     block_tile_prefix<kQuantSegCost, C::kThreads>(P, sm_prefix, sm_slot, reinterpret_cast<int*>(smem + C::kSmRed), cta == 0);
     prefix = sm_prefix;
-    slot_info = sm_slot;
+    if (P.max_pages <= (1 << 20)) slot_info = sm_slot;  // (lengths of 24 bits; longer ones come from the state)
   }
   Segment sg;
   const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;

@@ -295,6 +295,39 @@ def test_pages_behind_four_gigabytes():
     p.check()
 
 
+@pytest.mark.parametrize("stride,hq", [(1, 4), (4, 8)])
+def test_a_context_beyond_two_to_the_24_tokens(stride, hq):
+    """One page stands for all but the last of a context's pages, so that the plain statement can count its sixteen tokens as often."""
+    ctx, Q = (1 << 24) + 21, 2 * stride - 1
+    many = ctx // PAGE
+    p = Problem([ctx % PAGE + PAGE], [0], stride, hq, 1, seed=19, k_sigma=0.1)
+    last = p.table[0, 1:].copy()
+    table = np.concatenate([np.full(many, p.table[0, 0], np.int32), last])
+    p.to_gpu()
+    p.st["ctx_len"].fill_(ctx)
+    p.st["page_table"] = torch.from_numpy(table[None].copy()).to(DEV)
+    isd = isd_pkg.Isd(batch=1, stride=stride, n_q_heads=hq, n_kv_heads=1, vocab=64, max_pages_per_slot=len(table), num_pages=p.pages,
+                      logits_dtype="f32")
+    isd.isd_attn_quant(p.st, *p.dev, p.pool, p.out, p.lse)
+    assert isd.isd_read_status() == 0
+    K, V, n = p.slot_values(0)  # [1, 16 + 5 + n, 128]
+    weight = np.concatenate([np.full(PAGE, float(many)), np.ones(K.shape[1] - PAGE)])
+    out, lse = p.out[0].double().cpu().numpy(), p.lse[0].double().cpu().numpy()
+    x = p.q[0].double().numpy()
+    for r in range(n):
+        L = PAGE + ctx % PAGE + r + 1
+        a = x[r] @ K[0, :L].T * p.scale
+        e = np.exp(a - a.max(-1, keepdims=True)) * weight[:L]
+        t = e.sum(-1, keepdims=True)
+        want, wl = (e / t) @ V[0, :L], (a.max(-1, keepdims=True) + np.log(t))[:, 0]
+        mag = (np.abs(x[r]) @ np.abs(K[0, :L]).T).max(-1) * p.scale
+        # (a CTA's chain of additions is 2^24 / 148 keys long: 2^17 roundings of 2^-24 at most instead of 2^11, below 2^-7 in all)
+        to, tl = attention_bounds(want, wl, (e / t) @ np.abs(V[0, :L]), mag)
+        extra = 2.0 ** -7
+        assert (np.abs(out[r] - want) <= to + extra * ((e / t) @ np.abs(V[0, :L]))).all()
+        assert (np.abs(lse[r] - wl) <= tl + extra).all()
+
+
 def test_stream_repeat_and_captured_replay_give_the_same_bits():
     p = Problem([3000, 64, 900], [3, 0, 2], 4, 32, 8, seed=16).to_gpu()
     p.call()
