@@ -70,8 +70,9 @@ __device__ __forceinline__ QuantParam quant_param(float lo, float hi) {
 }
 
 // Eight codes clamp(round(x / s) + z, 0, 15), the i-th at bit shift(i) of the 64-bit result.  round() adds 1.5 * 2^23, where a
-// float's unit is 1; the clamp is taken there (bounds 1.5 * 2^23 - z and 15 more), and the codes, offset by the same
-// constant, are summed at their places and freed of it all at once.
+// float's unit is 1; the clamp is taken there (upper bound 1.5 * 2^23 - z + 15), and the codes, offset by the same constant, are
+// summed at their places and freed of it all at once.  Nothing falls below 0: x >= lo, so the rounded quotient is at least
+// that of lo, which is -z (rounding is symmetric, and -lo / s < 15.5, since s is (hi - lo) / 15 up to 2^-8 of it).
 template <class Shift>
 __device__ __forceinline__ uint2 quant_codes(const uint4& x, const QuantParam& p, Shift shift) {
   float f[8] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u),
@@ -89,7 +90,7 @@ __device__ __forceinline__ uint2 quant_codes(const uint4& x, const QuantParam& p
     }
     return make_uint2(out[0], out[1]);
   }
-  const float least = __uint_as_float(zero), most = __uint_as_float(zero + 15u);
+  const float most = __uint_as_float(zero + 15u);
   const uint64_t s2 = pack2(-p.s, -p.s), i2 = pack2(p.inv, p.inv), m2 = pack2(12582912.f, 12582912.f);
   uint32_t places[2] = {0u, 0u};
 #pragma unroll
@@ -97,8 +98,8 @@ __device__ __forceinline__ uint2 quant_codes(const uint4& x, const QuantParam& p
     const uint64_t v = pack2(f[i], f[i + 1]), q0 = mul2(v, i2);
     float a, b;
     unpack2(add2(fma2(fma2(q0, s2, v), i2, q0), m2), a, b);
-    a = fminf(fmaxf(a, least), most);
-    b = fminf(fmaxf(b, least), most);
+    a = fminf(a, most);
+    b = fminf(b, most);
     out[shift(i) >> 5] += __float_as_uint(a) << (shift(i) & 31);
     out[shift(i + 1) >> 5] += __float_as_uint(b) << (shift(i + 1) & 31);
     places[shift(i) >> 5] += 1u << (shift(i) & 31);
