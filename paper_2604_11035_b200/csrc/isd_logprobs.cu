@@ -364,18 +364,30 @@ __global__ void __launch_bounds__(kLpThreads, kLpPerSm) logprobs_kernel(const Lo
     if (!sm.last) return;
     __threadfence();
     if (tid == 0) P.ticket[entry] = 0;
-    M = -INFINITY;
-    for (int i = 0; i < P.pieces; ++i) M = fmaxf(M, __ldcg(&part[i].m));
-    s = w = 0.f;
-    for (int i = 0; i < P.pieces; ++i) {
-      const float d = (__ldcg(&part[i].m) - M) * P.scale2, f = lp_ex2(d), si = __ldcg(&part[i].s);
-      s = fmaf(si, f, s);
-      if (f > 0.f || f != f) w = fmaf(f, fmaf(d, si, __ldcg(&part[i].w)), w);
+    // a lane per piece (every warp for itself), the lists of a warp's share of the pieces: all in one trip to memory
+    const bool have = lane < P.pieces;
+    const float mi = have ? __ldcg(&part[lane].m) : -INFINITY, si = have ? __ldcg(&part[lane].s) : 0.f, wi = have ? __ldcg(&part[lane].w) : 0.f;
+    constexpr int kLists = kLpMaxPieces / kLpWarps;
+    u64 got[kLists];
+#pragma unroll
+    for (int k = 0; k < kLists; ++k) {
+      const int i = warp + k * kLpWarps;
+      got[k] = i < P.pieces && 31 - lane < P.top_n ? __ldcg(&part[i].key[31 - lane]) : 0ull;
+    }
+    M = lp_warp_max(mi);
+    const float d = (mi - M) * P.scale2, f = lp_ex2(d);
+    s = have ? si * f : 0.f;
+    w = have && (f > 0.f || f != f) ? f * fmaf(d, si, wi) : 0.f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, off);
+      w += __shfl_xor_sync(0xffffffffu, w, off);
     }
     if (P.top_n > 0) {
       list = 0;
-      for (int i = warp; i < P.pieces; i += kLpWarps)
-        list = warp_merge_desc(list, 31 - lane < P.top_n ? __ldcg(&part[i].key[31 - lane]) : 0ull);
+#pragma unroll
+      for (int k = 0; k < kLists; ++k)
+        if (warp + k * kLpWarps < P.pieces) list = warp_merge_desc(list, got[k]);
       list = block_merge_desc(list, sm.lists);
     }
   }
