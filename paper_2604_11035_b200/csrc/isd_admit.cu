@@ -30,8 +30,9 @@ struct AdmitParams {
   uint8_t* active;
   uint32_t* slot_status;
   int* mark;
-  // plan of the call for the second kernel: [0] admitted requests, [1] free pages before the call; then of the k-th admitted
-  // request: index, pages of the admitted ones before it (one more entry: of all)
+  // plan of the call for the second kernel: the k-th admitted request {index, slot, length, tokens before it}; the number of
+  // admitted requests and the free pages before the call; pages of the admitted ones before the k-th (one more entry: of all)
+  int4* plan_info;
   int* plan;
 };
 
@@ -81,8 +82,7 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
   const int top = *P.free_top;
   int64_t pages0 = 0, toks0 = 0;  // asked for by valid requests of earlier rounds
   int served_pages = 0, served_toks = 0, served = 0;
-  int* plan_req = P.plan + 2;
-  int* plan_page = plan_req + P.B;
+  int* plan_page = P.plan + 2;
   for (int base = 0; base < P.n; base += kAdmitThreads) {
     const int i = base + threadIdx.x;
     uint32_t why = 0;
@@ -117,7 +117,6 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
       P.result[i] = (int32_t)why;
       P.cu_len[i] = served_toks + my_t;
     }
-    served_toks += n_t;
     if (ok) {
       P.ctx_len[b] = len;
       P.n_ver[b] = 0;
@@ -125,9 +124,10 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
       P.slot_status[b] = 0;
       P.active[b] = 1;
       for (int m = 0; m < P.Q; ++m) P.block_tok[(size_t)b * P.Q + m] = m == 0 ? P.anchors[i] : P.mask_token;
-      plan_req[my_k] = i;
+      P.plan_info[my_k] = make_int4(i, b, len, served_toks + my_t);
       plan_page[my_k] = served_pages + my_p;
     }
+    served_toks += n_t;
     served += n_k;
     served_pages += n_p;
   }
@@ -148,17 +148,26 @@ __global__ void __launch_bounds__(kAdmitThreads) admit_plan_kernel(const AdmitPa
 // Page tables and maps: a half-warp per page, lane = token of the page.  The k-th page taken is free_stack[top - 1 - k]
 // whoever takes it (those served are a prefix of those who ask), so only the request of a page has to be found: by a search
 // once per kPagesEach pages, then by stepping on.
-constexpr int kPagesEach = 16;
+constexpr int kPagesEach = 16;  // (a lane each)
+constexpr int kSmemPlan = 1024;
 __global__ void __launch_bounds__(256) admit_maps_kernel(const AdmitParams P) {
   pdl_wait();
   pdl_launch_dependents();
+  __shared__ int sm_page[kSmemPlan + 1];
   const int served = P.plan[0], top = P.plan[1];
-  const int* plan_req = P.plan + 2;
-  const int* plan_page = plan_req + P.B;
+  const int* plan_page = P.plan + 2;
   if (served == 0) return;
+  if (served <= kSmemPlan) {  // the search below is a chain of loads: in shared memory it costs next to nothing
+    for (int i = threadIdx.x; i <= served; i += 256) sm_page[i] = plan_page[i];
+    __syncthreads();
+    plan_page = sm_page;
+  }
   const int pages = plan_page[served], off = threadIdx.x & 15;
+  const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
   const int group = (blockIdx.x * 256 + threadIdx.x) >> 4, groups = gridDim.x * 16;
   for (int k0 = group * kPagesEach; k0 < pages; k0 += groups * kPagesEach) {
+    // lane = page: one load for all of them, whose entries are handed round below
+    const int ids = k0 + off < pages ? P.free_stack[top - 1 - k0 - off] : 0;
     int lo = 0, hi = served;  // last request whose pages begin at or before k0 (every request takes at least one)
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -170,13 +179,14 @@ __global__ void __launch_bounds__(256) admit_maps_kernel(const AdmitParams P) {
         if (next >= 0) ++lo;
         first = plan_page[lo];
         next = plan_page[lo + 1];
-        req = plan_req[lo];
-        slot = P.slots[req];
-        len = P.lens[req];
-        cu = P.cu_len[req];
+        const int4 x = P.plan_info[lo];
+        req = x.x;
+        slot = x.y;
+        len = x.z;
+        cu = x.w;
       }
       const int j = k - first, pos = j * ISD_PAGE + off;
-      const int page = P.free_stack[top - 1 - k];
+      const int page = __shfl_sync(half, ids, k - k0, 16);
       if (off == 0) P.page_table[(size_t)slot * P.max_pages + j] = page;
       if (pos < len) {
         const int t = cu + pos;
@@ -193,7 +203,7 @@ __global__ void __launch_bounds__(256) admit_maps_kernel(const AdmitParams P) {
 int isd_admit_create(isd_ctx* ctx) {
   const size_t B = (size_t)ctx->cfg.batch;
   if (cudaMalloc(&ctx->admit_mark, sizeof(int) * B) != cudaSuccess) return ISD_ERR_NO_MEMORY;
-  if (cudaMalloc(&ctx->admit_plan, sizeof(int) * (2 * B + 3)) != cudaSuccess) return ISD_ERR_NO_MEMORY;
+  if (cudaMalloc(&ctx->admit_plan, sizeof(int4) * B + sizeof(int) * (B + 3)) != cudaSuccess) return ISD_ERR_NO_MEMORY;
   return cudaMemset(ctx->admit_mark, 0x7F, sizeof(int) * B) == cudaSuccess ? ISD_OK : ISD_ERR_CUDA;
 }
 
@@ -210,7 +220,7 @@ int isd_launch_admit(isd_ctx* ctx, isd_batch_state* st, const isd_admit_args* a,
   P.slot_map = a->slot_map; P.tok_req = a->tok_req; P.tok_pos = a->tok_pos;
   P.ctx_len = st->ctx_len; P.n_ver = st->n_ver; P.block_tok = st->block_tok; P.q_row0 = st->q_row0; P.page_table = st->page_table;
   P.free_stack = st->free_stack; P.free_top = st->free_top; P.active = st->active; P.slot_status = st->slot_status;
-  P.mark = ctx->admit_mark; P.plan = ctx->admit_plan;
+  P.mark = ctx->admit_mark; P.plan_info = reinterpret_cast<int4*>(ctx->admit_plan); P.plan = ctx->admit_plan + 4 * (size_t)c.batch;
   cudaError_t e = isd_launch_pdl(admit_plan_kernel, dim3(1), dim3(kAdmitThreads), 0, stream, P);
   ctx->launches++;
   if (e == cudaSuccess && a->n > 0) {

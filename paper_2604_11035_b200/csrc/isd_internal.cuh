@@ -78,7 +78,7 @@ struct isd_ctx {
   int* step_ticket;
   // ---- isd_admit
   int* admit_mark;       // [B] first request that names the slot (above every index between calls)
-  int* admit_plan;       // [2 + B + B + 1] the call's admitted requests
+  int* admit_plan;       // int4 [B], int [2 + B + 1]: the call's admitted requests
   // ---- isd_logprobs: partial results of rows cut into pieces, arrivals per row (zero between calls)
   void* lp_part;
   int* lp_ticket;
