@@ -7,6 +7,7 @@ library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 import torch
@@ -82,6 +83,7 @@ class IsdLogprobsArgs(C.Structure):
 
 
 _STATE_FIELDS = [n for n, _ in IsdBatchState._fields_]
+_state_tensors = operator.itemgetter(*_STATE_FIELDS)
 
 _lib = None
 
@@ -292,7 +294,7 @@ class Isd:
     # -- struct marshalling
     @staticmethod
     def state_struct(st: dict) -> IsdBatchState:
-        return IsdBatchState(*[_ptr(st[n]) for n in _STATE_FIELDS])
+        return IsdBatchState(*[t.data_ptr() if t is not None and t.is_cuda and t.is_contiguous() else _ptr(t) for t in _state_tensors(st)])
 
     @staticmethod
     def out_struct(out: dict) -> IsdVerifyOut:
@@ -395,14 +397,15 @@ class Isd:
         """Admit requests (slot, cached length, anchor token: int32 [n]) into inactive slots; `maps`: see alloc_admit_maps
         (slot_map, tok_req, tok_pos may be None)."""
         n, i32, dev = slots.numel(), torch.int32, self._dev
-        some = next((maps[k] for k in ("slot_map", "tok_req", "tok_pos") if maps.get(k) is not None), None)
+        slot_map, tok_req, tok_pos = maps.get("slot_map"), maps.get("tok_req"), maps.get("tok_pos")
+        some = slot_map if slot_map is not None else tok_req if tok_req is not None else tok_pos
         cap = 0x7FFFFFFF if some is None else some.numel()
         a = IsdAdmitArgs(_arg(slots, "slots", i32, (n,), dev), _arg(lens, "lens", i32, (n,), dev),
                          _arg(anchors, "anchors", i32, (n,), dev), _arg(maps["result"], "result", i32, (n,), dev),
                          _arg(maps["cu_len"], "cu_len", i32, (n + 1,), dev),
-                         _arg(maps.get("slot_map"), "slot_map", torch.int64, (cap,), dev),
-                         _arg(maps.get("tok_req"), "tok_req", i32, (cap,), dev),
-                         _arg(maps.get("tok_pos"), "tok_pos", i32, (cap,), dev), cap, n)
+                         _arg(slot_map, "slot_map", torch.int64, (cap,), dev),
+                         _arg(tok_req, "tok_req", i32, (cap,), dev),
+                         _arg(tok_pos, "tok_pos", i32, (cap,), dev), cap, n)
         s = self.state_struct(st)
         _check(self.lib.isd_admit(self.ctx, C.byref(s), C.byref(a), _stream()), "isd_admit")
 

@@ -94,7 +94,7 @@ def test_nothing_to_admit():
     b.admit([], [])
 
 
-@pytest.mark.parametrize("n,B", [(256, 300), (1024, 1100), (1500, 1500), (2500, 2600)])
+@pytest.mark.parametrize("n,B", [(256, 300), (1024, 1100), (1500, 1500), (2500, 2600), (1024, 4096), (70, 4097)])
 def test_many_requests(n, B):
     rng = np.random.default_rng(n)
     lens = rng.integers(0, 200, n)
