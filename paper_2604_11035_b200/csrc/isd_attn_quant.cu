@@ -651,7 +651,7 @@ __global__ void __launch_bounds__(Cfg<RMAX>::kThreads, 1) attn_quant_kernel(cons
         __syncwarp();
       }
     }
-    if (*S.abort_flag) {  // every issued copy must have landed before the CTA may exit
+    {  // every issued copy must have landed before the CTA may exit (they have, unless a wait ran out)
       for (uint32_t f = (n > (uint32_t)C::kStages ? n - C::kStages : 0); f < n; ++f)
         isd_bounded_wait(P.wait_ns, nullptr, [&]() { return mbar_try_wait(S.bar(C::FULL + f % C::kStages), (f / C::kStages) & 1u); });
     }
@@ -734,6 +734,11 @@ __global__ void __launch_bounds__(Cfg<RMAX>::kThreads, 1) attn_quant_kernel(cons
   __syncthreads();
   if (threadIdx.x == 0 && *S.abort_flag) atomicOr(P.global_status, ISD_ST_KERNEL_TIMEOUT);
   if (warp == C::kSoftmaxEnd) {
+    if (*S.abort_flag) {  // an MMA issued just before a wait ran out elsewhere has to end before tensor memory is given back: 50 us is many tiles' time
+      const unsigned long long t0 = isd_now_ns();
+      while (isd_now_ns() - t0 < 50000ull) {}
+      __syncwarp();
+    }
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(S.tmem) : "memory");
   }
